@@ -355,6 +355,102 @@ int slimdp_pull_local_step(slimdp_ctx* ctx, const float* w, uint64_t core_epoch,
                            float* const* w_local, const float* const* grad, float* const* delta, float eta,
                            uint32_t flags);
 
+/* ---------------------------------------------------------------------------------- */
+/* Operators of LocalTrain (section 3.3 step 1): what makes the gradient                 */
+/* ---------------------------------------------------------------------------------- */
+
+/* The gradient that slimdp_local_step takes comes from a forward and a backward pass over a worker's mini-batch.  The calls
+ * below are operators of such passes for models with layer norms, matrix products and a vocabulary: they read parameters
+ * from the workers' local models, serve all workers in one launch, and write every parameter's gradient in binary32 where
+ * slimdp_local_step and slimdp_local_step_pack read it.
+ *  - rows [host, n_workers]: rows (tokens) of each worker's mini-batch, <= SLIMDP_MAX_ROWS; 0 is allowed, the worker's matrices
+ *    may then be NULL, and its parameter gradients are written as sums over nothing.
+ *  - dtype: SLIMDP_F32, SLIMDP_F16 or SLIMDP_BF16, the type of everything given as void.  Vectors of parameters and all
+ *    gradients of parameters are binary32, pieces of the flat local model and gradient at any offset.
+ *  - A matrix is a [host table, n_workers] of [dev] row-major arrays, its rows ld elements apart (the same for all workers, at
+ *    least the row's length); any alignment that an element may have.  Elements between rows are neither read nor written.
+ *  - Sums, statistics and exponentials are binary32; results of a sixteen-bit type are rounded once, to nearest even.
+ *    Every sum has an order that depends on the sizes alone: same inputs, same bits.
+ *  - Outputs must not overlap inputs or each other, but for the cases each call names (the same array, the same ld).  Outputs of
+ *    different workers are different arrays; inputs (weights among them) may be shared.
+ *  - workspace [dev, aligned to 16 bytes]: scratch of at least the bytes that the *_workspace_bytes function gives for the same arguments
+ *    (0: may be NULL); the caller's, in use until the call's work on the stream is done.  Nothing else is allocated, and a call
+ *    may be recorded into a graph. */
+enum { SLIMDP_F32 = 0, SLIMDP_F16 = 1, SLIMDP_BF16 = 2 };
+#define SLIMDP_MAX_ROWS (1ull << 24)
+#define SLIMDP_MAX_NORM_COLS 65536ull
+#define SLIMDP_MAX_FEATURES (1ull << 20)
+#define SLIMDP_MAX_VOCAB (1ull << 24)
+#define SLIMDP_MAX_TEACHER 1024u
+/* Parameter gradients are added to what the arrays hold instead of replacing it: several calls for one gradient
+ * (a mini-batch in parts, weights used twice). */
+#define SLIMDP_GRAD_ACCUMULATE 1u
+
+/* Layer norm of every row: y = (x - mean) * rstd * weight + bias, mean over the row's cols elements, rstd = 1 / sqrt(var + eps),
+ * var = mean of (x - mean)^2.
+ *   x, y [rows, cols] (y may be x); weight, bias: NULL, or [host table] of (NULL or [dev, cols]) for 1 and 0;
+ *   eps positive and finite; mean, rstd: NULL or [host table] of [dev, rows], what the backward pass reads.
+ *   cols <= SLIMDP_MAX_NORM_COLS. */
+int slimdp_layer_norm(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* rows, uint64_t cols, uint32_t dtype, const void* const* x,
+                      uint64_t ldx, const float* const* weight, const float* const* bias, float eps, void* const* y, uint64_t ldy,
+                      float* const* mean, float* const* rstd);
+/* Its backward pass.  With xh = (x - mean) * rstd and a = weight * dy:
+ *     dx = rstd * (a - mean(a) - xh * mean(a * xh)),   dweight = sum over rows of dy * xh,   dbias = sum over rows of dy
+ *   mean, rstd as slimdp_layer_norm left them.  dx: NULL or a table (dx may be dy or x); dweight, dbias: NULL or a
+ *   table of (NULL or [dev, cols]); flags: SLIMDP_GRAD_ACCUMULATE (for dweight and dbias). */
+int slimdp_layer_norm_backward(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* rows, uint64_t cols, uint32_t dtype,
+                               const void* const* dy, uint64_t lddy, const void* const* x, uint64_t ldx, const float* const* weight,
+                               const float* const* mean, const float* const* rstd, void* const* dx, uint64_t lddx,
+                               float* const* dweight, float* const* dbias, uint32_t flags, void* workspace, uint64_t workspace_bytes);
+/* Workspace of slimdp_layer_norm_backward (none is needed where neither dweight nor dbias is asked for); 0 for invalid arguments.
+ * Pure host function. */
+uint64_t slimdp_layer_norm_workspace_bytes(uint32_t n_workers, const uint64_t* rows, uint64_t cols, uint32_t dtype);
+
+/* Matrix product with its epilogue:  z = x weight^T + bias,  y = activation(z) + residual.
+ *   x [rows, in]; weight [out, in] of the same type; bias: NULL or a table of (NULL or [dev, out]) binary32;
+ *   residual: NULL or [rows, out] (y may be residual); y [rows, out]; z: NULL or [rows, out], what the backward pass reads.
+ *   y is made from the z before it is rounded.  in, out <= SLIMDP_MAX_FEATURES. */
+enum { SLIMDP_ACT_NONE = 0, SLIMDP_ACT_RELU = 1, SLIMDP_ACT_GELU = 2 /* z * normal distribution function of z */,
+       SLIMDP_ACT_GELU_TANH = 3 /* 0.5 z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) */, SLIMDP_ACT_SILU = 4 /* z / (1 + exp(-z)) */ };
+int slimdp_linear(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* rows, uint64_t in, uint64_t out, uint32_t dtype,
+                  const void* const* x, uint64_t ldx, const void* const* weight, uint64_t ldw, const float* const* bias,
+                  uint32_t activation, const void* const* residual, uint64_t ldr, void* const* y, uint64_t ldy, void* const* z,
+                  uint64_t ldz, void* workspace, uint64_t workspace_bytes);
+/* Backward pass of the epilogue:  dz = dy * activation'(z),  dbias = sum over rows of dz (before dz is rounded).  The residual's gradient is
+ * dy itself.
+ *   dy, z [rows, out] (z: NULL with SLIMDP_ACT_NONE); dz: NULL or [rows, out] (dz may be dy or z); dbias: NULL or a table of
+ *   (NULL or [dev, out]); flags: SLIMDP_GRAD_ACCUMULATE (for dbias).  relu's slope at 0 is 0. */
+int slimdp_linear_epilogue_backward(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* rows, uint64_t out, uint32_t dtype,
+                                    const void* const* dy, uint64_t lddy, const void* const* z, uint64_t ldz, uint32_t activation,
+                                    void* const* dz, uint64_t lddz, float* const* dbias, uint32_t flags, void* workspace,
+                                    uint64_t workspace_bytes);
+/* Backward pass of the product:  dx = dz weight,  dweight = dz^T x.
+ *   dz [rows, out]; x [rows, in] (NULL without dweight); weight [out, in] (NULL without dx); dx: NULL or [rows, in];
+ *   dweight: NULL or [host table] of [dev, out * in] binary32; flags: SLIMDP_GRAD_ACCUMULATE (for dweight). */
+int slimdp_linear_backward(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* rows, uint64_t in, uint64_t out, uint32_t dtype,
+                           const void* const* dz, uint64_t lddz, const void* const* x, uint64_t ldx, const void* const* weight,
+                           uint64_t ldw, void* const* dx, uint64_t lddx, float* const* dweight, uint32_t flags, void* workspace,
+                           uint64_t workspace_bytes);
+/* Workspace of the three calls above, by pass; 0 for invalid arguments.  Pure host function. */
+enum { SLIMDP_LINEAR_FORWARD = 0, SLIMDP_LINEAR_EPILOGUE_BACKWARD = 1 /* in is not looked at, but valid */, SLIMDP_LINEAR_BACKWARD = 2 };
+uint64_t slimdp_linear_workspace_bytes(uint32_t n_workers, const uint64_t* rows, uint64_t in, uint64_t out, uint32_t dtype, uint32_t pass);
+
+/* Distillation from a teacher that sent its top logits as <index, value> pairs (the wire form of the explorer section of a pack,
+ * section 3.5): loss and gradient of the student's logits in one call.  Per row, with tau the temperature:
+ *     q = softmax(logits / tau) over the vocabulary,  p = softmax(value / tau) over the row's entries,  w = row_weight (1 if NULL)
+ *     lse = log sum exp(logits / tau),   loss = w tau^2 sum_j p_j (log p_j - log q[index_j]),   dlogits = w tau (q - sum_j p_j at index_j)
+ * The gradient is that of the sum of all rows' losses; w carries the loss's scale, a division by the number of tokens, a mask.
+ *   logits [rows, vocab]; index, value [rows, top], ldt elements apart, in any order; an index of 0xFFFFFFFF is no entry (lists shorter than
+ *   top); an index outside the vocabulary is taken as none and reported by slimdp_synchronize; one that appears twice counts twice.
+ *   A row without entries, or of weight 0, has loss 0 and gradient 0, whatever its logits hold.  An entry of value -inf has p = 0 and
+ *   adds nothing; a logit of -inf has q = 0, and an infinite loss where p > 0.  NaN values go through.
+ *   loss, lse: NULL or [host table] of [dev, rows]; dlogits: NULL or [rows, vocab] (dlogits may be logits).
+ *   vocab <= SLIMDP_MAX_VOCAB, top <= SLIMDP_MAX_TEACHER (0: no row has entries, index and value may be NULL); temperature positive and finite. */
+int slimdp_distill_loss(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* rows, uint64_t vocab, uint32_t dtype,
+                        const void* const* logits, uint64_t ldl, uint64_t top, const uint32_t* const* index, const float* const* value,
+                        uint64_t ldt, float temperature, const float* const* row_weight, float* const* loss, float* const* lse,
+                        void* const* dlogits, uint64_t lddl);
+
 /* Quantised wire values: the method composes with gradient quantisation (section 2.2, last sentences); the
  * comparison of section 4.2 uses random quantisation with 8 bits and buckets of 512, after Alistarh et al. (QSGD).
  * Applied to the packed values of workers worker0 .. worker0+n_workers-1 (kind 0: core_val, kind 1: expl_val):

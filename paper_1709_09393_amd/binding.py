@@ -29,6 +29,15 @@ SELECT_REUSE_HISTOGRAM = 1
 PACK_UPDATES_AS_SCORED = 1
 LOCAL_FIRST = 1
 QUANT_BUCKET = 512
+F32, F16, BF16 = 0, 1, 2
+GRAD_ACCUMULATE = 1
+MAX_ROWS = 1 << 24
+MAX_NORM_COLS = 65536
+MAX_FEATURES = 1 << 20
+MAX_VOCAB = 1 << 24
+MAX_TEACHER = 1024
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+LINEAR_FORWARD, LINEAR_EPILOGUE_BACKWARD, LINEAR_BACKWARD = 0, 1, 2
 
 EXPORTS = [
     "slimdp_create", "slimdp_destroy", "slimdp_workspace_bytes", "slimdp_capture_bytes", "slimdp_num_tiles",
@@ -36,7 +45,8 @@ EXPORTS = [
     "slimdp_score", "slimdp_dense_update_score", "slimdp_select_core", "slimdp_sample_explore", "slimdp_explore_hint", "slimdp_tile_offsets",
     "slimdp_pack", "slimdp_merge", "slimdp_pull", "slimdp_core_signature", "slimdp_debug_philox",
     "slimdp_select_core_static", "slimdp_import_core", "slimdp_local_step", "slimdp_local_step_pack", "slimdp_pull_local_step", "slimdp_quantize",
-    "slimdp_dequantize",
+    "slimdp_dequantize", "slimdp_layer_norm", "slimdp_layer_norm_backward", "slimdp_layer_norm_workspace_bytes", "slimdp_linear",
+    "slimdp_linear_epilogue_backward", "slimdp_linear_backward", "slimdp_linear_workspace_bytes", "slimdp_distill_loss",
 ]
 
 
@@ -120,6 +130,24 @@ def load() -> C.CDLL:
     L.slimdp_quantize.restype = C.c_int
     L.slimdp_dequantize.argtypes = [_vp, C.c_uint32, _vpp, _vpp, _u64p, _vpp]
     L.slimdp_dequantize.restype = C.c_int
+    u32, u64, f32 = C.c_uint32, C.c_uint64, C.c_float
+    L.slimdp_layer_norm.argtypes = [_vp, u32, _u64p, u64, u32, _vpp, u64, _vpp, _vpp, f32, _vpp, u64, _vpp, _vpp]
+    L.slimdp_layer_norm.restype = C.c_int
+    L.slimdp_layer_norm_backward.argtypes = [_vp, u32, _u64p, u64, u32, _vpp, u64, _vpp, u64, _vpp, _vpp, _vpp, _vpp, u64, _vpp, _vpp, u32,
+                                             _vp, u64]
+    L.slimdp_layer_norm_backward.restype = C.c_int
+    L.slimdp_layer_norm_workspace_bytes.argtypes = [u32, _u64p, u64, u32]
+    L.slimdp_layer_norm_workspace_bytes.restype = u64
+    L.slimdp_linear.argtypes = [_vp, u32, _u64p, u64, u64, u32, _vpp, u64, _vpp, u64, _vpp, u32, _vpp, u64, _vpp, u64, _vpp, u64, _vp, u64]
+    L.slimdp_linear.restype = C.c_int
+    L.slimdp_linear_epilogue_backward.argtypes = [_vp, u32, _u64p, u64, u32, _vpp, u64, _vpp, u64, u32, _vpp, u64, _vpp, u32, _vp, u64]
+    L.slimdp_linear_epilogue_backward.restype = C.c_int
+    L.slimdp_linear_backward.argtypes = [_vp, u32, _u64p, u64, u64, u32, _vpp, u64, _vpp, u64, _vpp, u64, _vpp, u64, _vpp, u32, _vp, u64]
+    L.slimdp_linear_backward.restype = C.c_int
+    L.slimdp_linear_workspace_bytes.argtypes = [u32, _u64p, u64, u64, u32, u32]
+    L.slimdp_linear_workspace_bytes.restype = u64
+    L.slimdp_distill_loss.argtypes = [_vp, u32, _u64p, u64, u32, _vpp, u64, u64, _vpp, _vpp, u64, f32, _vpp, _vpp, _vpp, _vpp, u64]
+    L.slimdp_distill_loss.restype = C.c_int
     _lib = L
     return L
 
@@ -407,6 +435,214 @@ class SlimDP:
         cnt = _u64arr([c.numel() for c in code])
         self._check(self._L.slimdp_dequantize(self._h, nw, _table(code), _table(scale), cnt, _table(out)))
         return out
+
+
+    # -- operators of LocalTrain ---------------------------------------------------------
+    # Lists hold one tensor a worker: matrices [rows of the worker, columns] with consecutive columns, rows any distance apart (the
+    # same for all workers); parameters of the local model and their gradients binary32 and contiguous (pieces of flat vectors).
+    def _layout(self, who: str, x: Sequence):
+        """(rows of every worker, columns, dtype number, torch dtype) from a call's first list."""
+        torch = self._torch
+        t = x[0]
+        if t.dim() != 2:
+            raise ValueError(f"{who}: expected one two-dimensional tensor a worker")
+        code = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}.get(t.dtype)
+        if code is None:
+            raise ValueError(f"{who}: unsupported dtype {t.dtype}")
+        return [v.shape[0] for v in x], t.shape[1], code, t.dtype
+
+    def _matrix(self, who: str, name: str, ts, rows, cols: int, dtype):
+        """Pointer table and row distance of a list of matrices; (None, 0) for none."""
+        if ts is None:
+            return None, 0
+        if len(ts) != len(rows):
+            raise ValueError(f"{who}: {name} holds {len(ts)} tensors for {len(rows)} workers")
+        table, ld = (C.c_void_p * len(ts))(), None
+        for q, t in enumerate(ts):
+            if t.dtype != dtype or t.dim() != 2 or t.shape[0] != rows[q] or t.shape[1] != cols or t.device != self.device:
+                raise ValueError(f"{who}: {name}[{q}] is {tuple(t.shape)} {t.dtype} on {t.device}, "
+                                 f"expected {(rows[q], cols)} {dtype} on {self.device}")
+            if rows[q] == 0:
+                continue
+            table[q] = t.data_ptr()
+            step, inner = t.stride()
+            if inner != 1 and cols > 1:
+                raise ValueError(f"{who}: columns of {name}[{q}] are not consecutive")
+            if rows[q] > 1:
+                if ld is None:
+                    ld = step
+                if step != ld or step < cols:
+                    raise ValueError(f"{who}: rows of {name}[{q}] are {step} elements apart, expected {max(ld, cols)}")
+        return table, ld or cols
+
+    def _vectors(self, who: str, name: str, ts, sizes, dtype):
+        """Pointer table of a list of contiguous tensors of the given numbers of elements; None for none, also for single workers."""
+        if ts is None:
+            return None
+        if len(ts) != len(sizes):
+            raise ValueError(f"{who}: {name} holds {len(ts)} tensors for {len(sizes)} workers")
+        table = (C.c_void_p * len(ts))()
+        for q, t in enumerate(ts):
+            if t is None:
+                continue
+            if t.dtype != dtype or t.numel() != sizes[q] or t.device != self.device or not t.is_contiguous():
+                raise ValueError(f"{who}: {name}[{q}] is {tuple(t.shape)} {t.dtype} on {t.device}, "
+                                 f"expected {sizes[q]} consecutive {dtype} on {self.device}")
+            table[q] = t.data_ptr() if sizes[q] else None
+        return table
+
+    def _new(self, make):
+        """Runs make with the context's stream current: memory goes back to the allocator in the order of that stream's work."""
+        torch = self._torch
+        if torch.cuda.current_device() == self.device.index and torch.cuda.current_stream().cuda_stream == self.stream.cuda_stream:
+            return make()
+        with torch.cuda.device(self.device), torch.cuda.stream(self.stream):
+            return make()
+
+    def _workspace(self, nbytes: int):
+        """Scratch for one call; the tensor is to live until the call is enqueued."""
+        if not nbytes:
+            return None
+        return self._new(lambda: self._torch.empty(nbytes, dtype=self._torch.uint8, device=self.device))
+
+    def _matrices(self, rows, cols: int, dtype):
+        return self._new(lambda: [self._torch.empty((r, cols), dtype=dtype, device=self.device) for r in rows])
+
+    def _flat(self, sizes, dtype=None):
+        return self._new(lambda: [self._torch.empty(n, dtype=dtype or self._torch.float32, device=self.device) for n in sizes])
+
+    def layer_norm(self, x: Sequence, weight: Optional[Sequence], bias: Optional[Sequence], eps: float = 1e-5, y: Optional[List] = None,
+                   mean: Optional[List] = None, rstd: Optional[List] = None):
+        """Layer norm of every worker's rows; returns (y, mean, rstd), the latter two for the backward pass."""
+        who, f32 = "layer_norm", self._torch.float32
+        rows, cols, code, dtype = self._layout(who, x)
+        if y is None:
+            y = self._matrices(rows, cols, dtype)
+        if mean is None:
+            mean = self._flat(rows)
+        if rstd is None:
+            rstd = self._flat(rows)
+        px, ldx = self._matrix(who, "x", x, rows, cols, dtype)
+        py, ldy = self._matrix(who, "y", y, rows, cols, dtype)
+        per = [cols] * len(rows)
+        self._check(self._L.slimdp_layer_norm(self._h, len(rows), _u64arr(rows), cols, code, px, ldx, self._vectors(who, "weight", weight, per, f32),
+                                              self._vectors(who, "bias", bias, per, f32), eps, py, ldy,
+                                              self._vectors(who, "mean", mean, rows, f32), self._vectors(who, "rstd", rstd, rows, f32)))
+        return y, mean, rstd
+
+    def layer_norm_backward(self, dy: Sequence, x: Sequence, weight: Optional[Sequence], mean: Sequence, rstd: Sequence,
+                            dx: Optional[List] = None, dweight: Optional[List] = None, dbias: Optional[List] = None,
+                            accumulate: bool = False, want_dx: bool = True, want_params: bool = True):
+        """Gradients of layer_norm(): returns (dx, dweight, dbias), None for what is neither given nor wanted."""
+        who, f32 = "layer_norm_backward", self._torch.float32
+        rows, cols, code, dtype = self._layout(who, x)
+        per = [cols] * len(rows)
+        if dx is None and want_dx:
+            dx = self._matrices(rows, cols, dtype)
+        if want_params and not accumulate:
+            dweight = dweight if dweight is not None else self._flat(per)
+            dbias = dbias if dbias is not None else self._flat(per)
+        pdy, lddy = self._matrix(who, "dy", dy, rows, cols, dtype)
+        px, ldx = self._matrix(who, "x", x, rows, cols, dtype)
+        pdx, lddx = self._matrix(who, "dx", dx, rows, cols, dtype)
+        n = _u64arr(rows)
+        ws = self._workspace(self._L.slimdp_layer_norm_workspace_bytes(len(rows), n, cols, code) if dweight is not None or dbias is not None else 0)
+        self._check(self._L.slimdp_layer_norm_backward(
+            self._h, len(rows), n, cols, code, pdy, lddy, px, ldx, self._vectors(who, "weight", weight, per, f32),
+            self._vectors(who, "mean", mean, rows, f32), self._vectors(who, "rstd", rstd, rows, f32), pdx, lddx,
+            self._vectors(who, "dweight", dweight, per, f32), self._vectors(who, "dbias", dbias, per, f32),
+            GRAD_ACCUMULATE if accumulate else 0, _ptr(ws), ws.numel() if ws is not None else 0))
+        return dx, dweight, dbias
+
+    def linear(self, x: Sequence, weight: Sequence, bias: Optional[Sequence] = None, activation: str = "none",
+               residual: Optional[Sequence] = None, y: Optional[List] = None, z: Optional[List] = None, keep: bool = False):
+        """activation(x weight^T + bias) + residual; returns (y, z), z (before the activation, for the backward pass) if given or keep."""
+        who, f32 = "linear", self._torch.float32
+        rows, cols, code, dtype = self._layout(who, x)
+        out = weight[0].shape[0]
+        if y is None:
+            y = self._matrices(rows, out, dtype)
+        if z is None and keep:
+            z = self._matrices(rows, out, dtype)
+        outs = [out] * len(rows)
+        px, ldx = self._matrix(who, "x", x, rows, cols, dtype)
+        pw, ldw = self._matrix(who, "weight", weight, outs, cols, dtype)
+        pr, ldr = self._matrix(who, "residual", residual, rows, out, dtype)
+        py, ldy = self._matrix(who, "y", y, rows, out, dtype)
+        pz, ldz = self._matrix(who, "z", z, rows, out, dtype)
+        n = _u64arr(rows)
+        ws = self._workspace(self._L.slimdp_linear_workspace_bytes(len(rows), n, cols, out, code, LINEAR_FORWARD))
+        self._check(self._L.slimdp_linear(self._h, len(rows), n, cols, out, code, px, ldx, pw, ldw, self._vectors(who, "bias", bias, outs, f32),
+                                          ACTIVATIONS[activation], pr, ldr, py, ldy, pz, ldz, _ptr(ws), ws.numel() if ws is not None else 0))
+        return y, z
+
+    def linear_epilogue_backward(self, dy: Sequence, z: Optional[Sequence] = None, activation: str = "none", dz: Optional[List] = None,
+                                 dbias: Optional[List] = None, accumulate: bool = False, want_dbias: bool = True):
+        """Gradients of linear()'s epilogue: returns (dz, dbias).  Without an activation dz is dy, and none is written unless given."""
+        who, f32 = "linear_epilogue_backward", self._torch.float32
+        rows, out, code, dtype = self._layout(who, dy)
+        per = [out] * len(rows)
+        if dz is None and activation != "none":
+            dz = self._matrices(rows, out, dtype)
+        if dbias is None and want_dbias and not accumulate:
+            dbias = self._flat(per)
+        pdy, lddy = self._matrix(who, "dy", dy, rows, out, dtype)
+        pz, ldz = self._matrix(who, "z", z if activation != "none" else None, rows, out, dtype)
+        pdz, lddz = self._matrix(who, "dz", dz, rows, out, dtype)
+        n = _u64arr(rows)
+        ws = self._workspace(self._L.slimdp_linear_workspace_bytes(len(rows), n, 1, out, code, LINEAR_EPILOGUE_BACKWARD) if dbias is not None else 0)
+        self._check(self._L.slimdp_linear_epilogue_backward(self._h, len(rows), n, out, code, pdy, lddy, pz, ldz, ACTIVATIONS[activation],
+                                                            pdz, lddz, self._vectors(who, "dbias", dbias, per, f32),
+                                                            GRAD_ACCUMULATE if accumulate else 0, _ptr(ws), ws.numel() if ws is not None else 0))
+        return (dz if dz is not None else dy), dbias
+
+    def linear_backward(self, dz: Sequence, x: Optional[Sequence], weight: Optional[Sequence], dx: Optional[List] = None,
+                        dweight: Optional[List] = None, accumulate: bool = False, want_dx: bool = True, want_dweight: bool = True):
+        """Gradients of linear()'s product: returns (dx, dweight), None for what is neither given nor wanted."""
+        who, f32 = "linear_backward", self._torch.float32
+        rows, out, code, dtype = self._layout(who, dz)
+        cols = (x if x is not None else weight)[0].shape[1]
+        W = len(rows)
+        if dx is None and want_dx:
+            dx = self._matrices(rows, cols, dtype)
+        if dweight is None and want_dweight and not accumulate:
+            dweight = [v.view(out, cols) for v in self._flat([out * cols] * W)]
+        pdz, lddz = self._matrix(who, "dz", dz, rows, out, dtype)
+        px, ldx = self._matrix(who, "x", x, rows, cols, dtype)
+        pw, ldw = self._matrix(who, "weight", weight, [out] * W, cols, dtype)
+        pdx, lddx = self._matrix(who, "dx", dx, rows, cols, dtype)
+        n = _u64arr(rows)
+        ws = self._workspace(self._L.slimdp_linear_workspace_bytes(W, n, cols, out, code, LINEAR_BACKWARD))
+        self._check(self._L.slimdp_linear_backward(self._h, W, n, cols, out, code, pdz, lddz, px, ldx, pw, ldw, pdx, lddx,
+                                                   self._vectors(who, "dweight", dweight, [out * cols] * W, f32),
+                                                   GRAD_ACCUMULATE if accumulate else 0, _ptr(ws), ws.numel() if ws is not None else 0))
+        return dx, dweight
+
+    def distill_loss(self, logits: Sequence, index: Sequence, value: Sequence, temperature: float = 1.0,
+                     row_weight: Optional[Sequence] = None, loss: Optional[List] = None, lse: Optional[List] = None,
+                     dlogits: Optional[List] = None, want_grad: bool = True):
+        """Distillation from the teacher's top logits (int32 index, -1 = no entry; binary32 value): returns (loss, lse, dlogits), dlogits
+        None if neither given nor wanted."""
+        who, torch = "distill_loss", self._torch
+        rows, vocab, code, dtype = self._layout(who, logits)
+        top = index[0].shape[1]
+        if loss is None:
+            loss = self._flat(rows)
+        if lse is None:
+            lse = self._flat(rows)
+        if dlogits is None and want_grad:
+            dlogits = self._matrices(rows, vocab, dtype)
+        pl, ldl = self._matrix(who, "logits", logits, rows, vocab, dtype)
+        pi, ldt = self._matrix(who, "index", index, rows, top, torch.int32)
+        pv, ldv = self._matrix(who, "value", value, rows, top, torch.float32)
+        if ldt != ldv:
+            raise ValueError(f"{who}: rows of index and value lie {ldt} and {ldv} elements apart")
+        pd, lddl = self._matrix(who, "dlogits", dlogits, rows, vocab, dtype)
+        self._check(self._L.slimdp_distill_loss(self._h, len(rows), _u64arr(rows), vocab, code, pl, ldl, top, pi, pv, ldt, temperature,
+                                                self._vectors(who, "row_weight", row_weight, rows, torch.float32),
+                                                self._vectors(who, "loss", loss, rows, torch.float32),
+                                                self._vectors(who, "lse", lse, rows, torch.float32), pd, lddl))
+        return loss, lse, dlogits
 
 
 def wire_bytes(k: int, m: int, quantized: bool) -> int:

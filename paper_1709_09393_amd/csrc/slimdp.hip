@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "slimdp.h"
+#include "slimdp_host.h"
 #include "slimdp_kernels.h"
 #include "slimdp_core.h"
 #include "slimdp_explore.h"
@@ -663,6 +664,19 @@ int explorer_plan(slimdp_ctx* ctx, const char* who, const uint64_t* k_seg, const
 
 }  // namespace
 
+// What the other translation unit sees of a context.
+HostView slimdp::host_view(const slimdp_ctx* c) { return {c->maxW, c->device, c->stream, c->d_flags + 1}; }
+
+int slimdp::host_fail(slimdp_ctx* c, int code, const char* fmt, ...)
+{
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    return fail(c, code, "%s", buf);
+}
+
 extern "C" {
 
 uint64_t slimdp_num_tiles(uint64_t n, uint32_t n_seg, const uint64_t* seg_off)
@@ -871,9 +885,10 @@ int slimdp_synchronize(slimdp_ctx* ctx)
     SLIMDP_HIP(ctx, hipMemcpy(flags, ctx->d_flags, sizeof flags, hipMemcpyDeviceToHost));
     if (flags[1]) {
         SLIMDP_HIP(ctx, hipMemset(ctx->d_flags + 1, 0, 4));
-        return fail(ctx, SLIMDP_ERR_DEVICE_STATUS, "device status 0x%x:%s%s", flags[1],
+        return fail(ctx, SLIMDP_ERR_DEVICE_STATUS, "device status 0x%x:%s%s%s", flags[1],
                     (flags[1] & 1u) ? " an emitted index list does not have the requested length;" : "",
-                    (flags[1] & 2u) ? " a segment holds fewer eligible parameters than requested;" : "");
+                    (flags[1] & 2u) ? " a segment holds fewer eligible parameters than requested;" : "",
+                    (flags[1] & STATUS_TEACHER) ? " a teacher's index lies outside the vocabulary;" : "");
     }
     return SLIMDP_OK;
 }

@@ -1,0 +1,243 @@
+// Matrix products of the worker side: x W^T with bias, activation and residual in the epilogue, and the two products that are its
+// gradients.  Included only by slimdp_train.hip.
+#pragma once
+#include <type_traits>
+
+#include "slimdp_train.h"
+#include "slimdp_norm.h"
+
+namespace slimdp {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// C[m][n] = sum over k of A(m, k) B(n, k) for every worker.  An operand lies either with k running (rows of m or n) or with m or n
+// running (rows of k: KROWS).
+struct GemmArgs {
+    InTab a, b, bias, residual;
+    OutTab c, z;
+    RowTab rows;                 // per worker: M, or with k_is_rows the length of the sum
+    uint32_t M, N, K;            // the largest of the workers where it varies
+    int k_is_rows;
+    uint64_t lda, ldb, ldc, ldr, ldz;
+    uint32_t splits, k_split;    // the sum in pieces of k_split (a multiple of the step), one block each
+    float* partial;              // [worker][split][M][N] where splits > 1
+    int act, accumulate;
+};
+
+// 16 bytes of either operand a lane: eight products' steps of sixteen-bit elements in one instruction, four of binary32 in one each.
+template <class T> struct Mma;
+template <> struct Mma<_Float16> {
+    static __device__ __forceinline__ f32x4 step(raw4 a, raw4 b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
+};
+template <> struct Mma<__bf16> {
+    static __device__ __forceinline__ f32x4 step(raw4 a, raw4 b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+};
+template <> struct Mma<float> {
+    // the four steps take the elements k, k + 4, k + 8, k + 12 of sixteen, the same ones of both operands
+    static __device__ __forceinline__ f32x4 step(raw4 a, raw4 b, f32x4 c)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[i]), __uint_as_float(b[i]), c, 0, 0, 0);
+        return c;
+    }
+};
+
+// N by N elements, a vector of sixteen bytes a row, turned over.
+template <class T> __device__ __forceinline__ void transpose(raw4 (&v)[Vec<T>::N])
+{
+    constexpr int N = Vec<T>::N;
+    raw4 o[N];
+    if constexpr (N == 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[i][j] = v[j][i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                o[i][j] = __builtin_amdgcn_perm(v[2 * j + 1][i >> 1], v[2 * j][i >> 1], (i & 1) ? 0x07060302u : 0x05040100u);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = o[i];
+}
+
+// What becomes of four consecutive columns of one row of the sum.
+//   EPI 0: z = sum + bias, c = act(z) + residual, both in T      EPI 1: c = sum in T      EPI 2: c = sum in binary32, or c + sum
+template <class T, int EPI>
+__device__ __forceinline__ void epilogue4(const GemmArgs& a, uint32_t q, uint32_t m, uint32_t n, uint32_t N, const float s[4])
+{
+    float v[4] = {s[0], s[1], s[2], s[3]};
+    const bool full = n + 4 <= N;
+    if constexpr (EPI == 2) {
+        float* c = static_cast<float*>(a.c.p[q]) + (size_t)m * a.ldc + n;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (full || n + i < N) c[i] = a.accumulate ? c[i] + v[i] : v[i];
+    } else {
+        if constexpr (EPI == 0) {
+            const float* bias = static_cast<const float*>(a.bias.p[q]);
+            T* z = static_cast<T*>(a.z.p[q]);
+            const T* res = static_cast<const T*>(a.residual.p[q]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (!full && n + i >= N) break;
+                if (bias) v[i] += bias[n + i];
+                if (z) z[(size_t)m * a.ldz + n + i] = (T)v[i];
+                v[i] = act_value(v[i], a.act);
+                if (res) v[i] += (float)res[(size_t)m * a.ldr + n + i];
+            }
+        }
+        T* c = static_cast<T*>(a.c.p[q]) + (size_t)m * a.ldc + n;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (full || n + i < N) c[i] = (T)v[i];
+    }
+}
+
+// 128 x 128 of C a block of four waves (64 x 64 each, sixteen 16 x 16 accumulators), 128 bytes of k a step.  The next step's
+// pieces are loaded into registers while this one's are multiplied from shared memory; there either operand lies with k running,
+// 128 bytes a row, its eight vectors exchanged by the row's number so that the sixteen rows that a read touches meet
+// different banks.  Operands with rows of k are turned over in registers on the way.  Any size, stride and alignment: what lies
+// outside reads as zero.
+// grid (tiles, 1, workers * splits)
+template <class T, bool AK, bool BK_, int EPI>
+__global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
+{
+    constexpr uint32_t V = Vec<T>::N, BM = 128, BN = 128, BK = 8 * V;
+    __shared__ raw4 sa[BM * 8], sb[BN * 8];
+    const uint32_t q = blockIdx.z / a.splits, split = blockIdx.z % a.splits;
+    const uint32_t M = a.k_is_rows ? a.M : a.rows.n[q], N = a.N, Kall = a.k_is_rows ? a.rows.n[q] : a.K;
+    const uint32_t across = (N + BN - 1) / BN, m0 = blockIdx.x / across * BM, n0 = blockIdx.x % across * BN;
+    if (m0 >= M) return;
+    const uint32_t k0 = min(Kall, split * a.k_split), K = min(Kall, k0 + a.k_split);
+    const T* A = static_cast<const T*>(a.a.p[q]);
+    const T* B = static_cast<const T*>(a.b.p[q]);
+    const uint32_t t = threadIdx.x, lane = t & 63u, wave = t >> 6, wm = wave >> 1, wn = wave & 1u;
+
+    // one operand's pieces of a step: four vectors a thread with k running, one square of V x V elements otherwise
+    constexpr uint32_t SQ = BM / V * 8;                            // squares of a tile: 128 or 256
+    constexpr int RA = AK ? (int)V : 4, RB = BK_ ? (int)V : 4;
+    raw4 ra[RA], rb[RB];
+    auto load = [&](auto krows, const T* P, uint64_t ld, uint32_t x0, uint32_t X, uint32_t kb, uint32_t tt, auto& reg) {
+        if constexpr (!decltype(krows)::value) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t x = x0 + (t >> 3) + 32u * i, k = kb + (t & 7u) * V;
+                reg[i] = x < X && k < K ? load_clip(P + (size_t)x * ld, k, K) : raw4{0, 0, 0, 0};
+            }
+        } else {
+            const uint32_t x = x0 + (tt % (BM / V)) * V, kr = kb + (tt / (BM / V)) * V;
+#pragma unroll
+            for (uint32_t i = 0; i < V; ++i)
+                reg[i] = tt < SQ && x < X && kr + i < K ? load_clip(P + (size_t)(kr + i) * ld, x, X) : raw4{0, 0, 0, 0};
+        }
+    };
+    auto put = [&](auto krows, raw4* s, uint32_t tt, auto& reg) {
+        if constexpr (!decltype(krows)::value) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t x = (t >> 3) + 32u * i;
+                s[x * 8 + ((t & 7u) ^ (x & 7u))] = reg[i];
+            }
+        } else if (tt < SQ) {
+            transpose<T>(reg);
+            const uint32_t x = (tt % (BM / V)) * V, ck = tt / (BM / V);
+#pragma unroll
+            for (uint32_t i = 0; i < V; ++i) s[(x + i) * 8 + (ck ^ ((x + i) & 7u))] = reg[i];
+        }
+    };
+    typedef std::integral_constant<bool, AK> ak_t;
+    typedef std::integral_constant<bool, BK_> bk_t;
+    // where squares occupy half of the block, the second operand's go to the other half
+    const uint32_t ta = t, tb = SQ < 256 && AK ? (t + 128u) & 255u : t;
+    f32x4 acc[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (k0 < K) {
+        load(ak_t{}, A, a.lda, m0, M, k0, ta, ra);
+        load(bk_t{}, B, a.ldb, n0, N, k0, tb, rb);
+    }
+    for (uint32_t kb = k0; kb < K; kb += BK) {
+        __syncthreads();
+        put(ak_t{}, sa, ta, ra);
+        put(bk_t{}, sb, tb, rb);
+        __syncthreads();
+        if (kb + BK < K) {
+            load(ak_t{}, A, a.lda, m0, M, kb + BK, ta, ra);
+            load(bk_t{}, B, a.ldb, n0, N, kb + BK, tb, rb);
+        }
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            raw4 fa[4], fb[4];
+            const uint32_t ch = ks * 4 + (lane >> 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t xa = wm * 64 + i * 16 + (lane & 15u), xb = wn * 64 + i * 16 + (lane & 15u);
+                fa[i] = sa[xa * 8 + (ch ^ (xa & 7u))];
+                fb[i] = sb[xb * 8 + (ch ^ (xb & 7u))];
+            }
+            // B first: a lane then holds four consecutive columns of one row of C
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[i][j] = Mma<T>::step(fb[j], fa[i], acc[i][j]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t m = m0 + wm * 64 + i * 16 + (lane & 15u);
+        if (m >= M) continue;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t n = n0 + wn * 64 + j * 16 + (lane >> 4) * 4;
+            if (n >= N) continue;
+            const float s[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+            if (a.splits == 1) epilogue4<T, EPI>(a, q, m, n, N, s);
+            else {
+                float* p = a.partial + (((size_t)q * a.splits + split) * a.M + m) * N + n;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (n + e < N) p[e] = s[e];
+            }
+        }
+    }
+}
+
+// The pieces of split sums, added in order, and the epilogue.  grid (blocks, rows in turn, workers)
+template <class T, int EPI>
+__global__ __launch_bounds__(256) void k_gemm_join(GemmArgs a)
+{
+    const uint32_t q = blockIdx.z, M = a.k_is_rows ? a.M : a.rows.n[q], N = a.N;
+    const uint32_t n = (blockIdx.x * 256 + threadIdx.x) * 4;
+    if (n >= N) return;
+    for (uint32_t m = blockIdx.y; m < M; m += gridDim.y) {
+        float s[4] = {0.f, 0.f, 0.f, 0.f};
+        for (uint32_t p = 0; p < a.splits; ++p) {
+            const float* src = a.partial + (((size_t)q * a.splits + p) * a.M + m) * N + n;
+            if (n + 4 <= N) {
+                const raw4 v = load_raw<float>(src);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[e] += __uint_as_float(v[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (n + e < N) s[e] += src[e];
+            }
+        }
+        epilogue4<T, EPI>(a, q, m, n, N, s);
+    }
+}
+
+}  // namespace slimdp

@@ -1,0 +1,510 @@
+// libslimdp, the worker side's training operators (layer norm, matrix product with epilogue, distillation loss, each with its
+// gradients): argument checks and launches.  The kernels are in slimdp_norm.h, slimdp_linear.h and slimdp_distill.h.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <type_traits>
+
+#include "slimdp.h"
+#include "slimdp_host.h"
+#include "slimdp_norm.h"
+#include "slimdp_linear.h"
+#include "slimdp_distill.h"
+
+using namespace slimdp;
+
+namespace {
+
+constexpr uint64_t LD_MAX = 1ull << 32;
+
+// The context's device for the length of a call, whichever is current.
+struct OnDevice {
+    int before = -1;
+    hipError_t e;
+    explicit OnDevice(int device)
+    {
+        e = hipGetDevice(&before);
+        if (e == hipSuccess && before != device) e = hipSetDevice(device); else before = -1;
+    }
+    ~OnDevice() { if (before >= 0) (void)hipSetDevice(before); }
+};
+
+struct Call {
+    slimdp_ctx* ctx;
+    const char* who;
+    HostView v{};
+    uint32_t W = 0;
+    const uint64_t* rows = nullptr;
+    uint64_t most = 0;               // rows of the worker that has most
+    RowTab tab{};
+    int rc = SLIMDP_OK;
+
+    bool ok() const { return rc == SLIMDP_OK; }
+    size_t esize = 4;
+
+    int begin(slimdp_ctx* c, const char* name, uint32_t n_workers, const uint64_t* r, uint32_t dtype)
+    {
+        ctx = c;
+        who = name;
+        if (!c) return rc = SLIMDP_ERR_INVALID_ARG;
+        v = host_view(c);
+        W = n_workers;
+        if (W == 0 || W > v.max_workers)
+            return rc = host_fail(c, SLIMDP_ERR_INVALID_ARG, "%s: n_workers=%u outside [1, %u]", who, W, v.max_workers);
+        if (!r) return rc = host_fail(c, SLIMDP_ERR_INVALID_ARG, "%s: rows is NULL", who);
+        if (dtype > SLIMDP_BF16) return rc = host_fail(c, SLIMDP_ERR_INVALID_ARG, "%s: unknown dtype %u", who, dtype);
+        esize = dtype == SLIMDP_F32 ? 4 : 2;
+        rows = r;
+        for (uint32_t q = 0; q < W; ++q) {
+            if (r[q] > SLIMDP_MAX_ROWS)
+                return rc = host_fail(c, SLIMDP_ERR_OUT_OF_RANGE, "%s: rows[%u] exceeds %llu", who, q, (unsigned long long)SLIMDP_MAX_ROWS);
+            tab.n[q] = (uint32_t)r[q];
+            most = std::max(most, r[q]);
+        }
+        return rc;
+    }
+    void size(const char* what, uint64_t n, uint64_t max)
+    {
+        if (!ok()) return;
+        if (n == 0) rc = host_fail(ctx, SLIMDP_ERR_INVALID_ARG, "%s: %s is 0", who, what);
+        else if (n > max) rc = host_fail(ctx, SLIMDP_ERR_OUT_OF_RANGE, "%s: %s exceeds %llu", who, what, (unsigned long long)max);
+    }
+    // A table of matrices with a row each of a worker's rows (their entries may be NULL where there are none).
+    template <class P> void matrix(const char* what, P const* t, uint64_t ld, uint64_t cols, size_t es, bool optional = false)
+    {
+        if (!ok() || (!t && optional)) return;
+        if (!t) { rc = host_fail(ctx, SLIMDP_ERR_INVALID_ARG, "%s: %s is NULL", who, what); return; }
+        if (ld < cols || ld > LD_MAX) {
+            rc = host_fail(ctx, SLIMDP_ERR_INVALID_ARG, "%s: rows of %s are %llu apart, with %llu elements each", who, what,
+                           (unsigned long long)ld, (unsigned long long)cols);
+            return;
+        }
+        for (uint32_t q = 0; q < W; ++q) entry(what, q, t[q], es, rows[q] != 0);
+    }
+    // A table of parameter vectors or matrices (needed whatever the rows); optional: the table, or single entries.
+    template <class P> void params(const char* what, P const* t, size_t es, bool optional)
+    {
+        if (!ok() || (!t && optional)) return;
+        if (!t) { rc = host_fail(ctx, SLIMDP_ERR_INVALID_ARG, "%s: %s is NULL", who, what); return; }
+        for (uint32_t q = 0; q < W; ++q) entry(what, q, t[q], es, !optional);
+    }
+    void entry(const char* what, uint32_t q, const void* p, size_t es, bool needed)
+    {
+        if (!ok()) return;
+        if (!p && needed) rc = host_fail(ctx, SLIMDP_ERR_INVALID_ARG, "%s: %s[%u] is NULL", who, what, q);
+        else if (reinterpret_cast<uintptr_t>(p) % es) rc = host_fail(ctx, SLIMDP_ERR_INVALID_ARG, "%s: %s[%u] is not aligned to its elements", who, what, q);
+    }
+    // Outputs that may not be the given input; same: unless rows lie the same distance apart.
+    template <class P, class R> void apart(const char* wa, P const* a, const char* wb, R const* b, bool same = false)
+    {
+        if (!ok() || !a || !b || same) return;
+        for (uint32_t q = 0; q < W; ++q)
+            for (uint32_t o = 0; o < W; ++o)
+                if (a[q] && rows[q] && rows[o] && static_cast<const void*>(a[q]) == static_cast<const void*>(b[o])) {
+                    rc = host_fail(ctx, SLIMDP_ERR_INVALID_ARG, "%s: %s[%u] is %s[%u]", who, wa, q, wb, o);
+                    return;
+                }
+    }
+    // Outputs of different workers are different arrays.
+    template <class P> void distinct(const char* what, P const* t, bool per_row)
+    {
+        if (!ok() || !t) return;
+        for (uint32_t q = 0; q < W; ++q)
+            for (uint32_t o = 0; o < q; ++o)
+                if (t[q] && t[q] == t[o] && (!per_row || (rows[q] && rows[o]))) {
+                    rc = host_fail(ctx, SLIMDP_ERR_INVALID_ARG, "%s: %s[%u] is %s[%u]", who, what, o, what, q);
+                    return;
+                }
+    }
+    void workspace(void* ws, uint64_t have, uint64_t need)
+    {
+        if (!ok() || need == 0) return;
+        if (!ws || have < need)
+            rc = host_fail(ctx, SLIMDP_ERR_WORKSPACE, "%s: needs a workspace of %llu bytes, got %llu", who, (unsigned long long)need,
+                           (unsigned long long)(ws ? have : 0));
+        else if (reinterpret_cast<uintptr_t>(ws) % 16) rc = host_fail(ctx, SLIMDP_ERR_INVALID_ARG, "%s: workspace is not aligned to 16 bytes", who);
+    }
+    template <class P> InTab in(P const* t) const
+    {
+        InTab r;
+        for (int q = 0; q < MAXW_T; ++q) r.p[q] = t && q < (int)W ? t[q] : nullptr;
+        return r;
+    }
+    template <class P> OutTab out(P const* t) const
+    {
+        OutTab r;
+        for (int q = 0; q < MAXW_T; ++q) r.p[q] = t && q < (int)W ? t[q] : nullptr;
+        return r;
+    }
+    template <class F> int launched(const char* name, F&& f)
+    {
+        OnDevice dev(v.device);
+        if (dev.e != hipSuccess) return rc = host_fail(ctx, SLIMDP_ERR_HIP, "%s: hipSetDevice: %s", who, hipGetErrorString(dev.e));
+        f();
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) rc = host_fail(ctx, SLIMDP_ERR_HIP, "%s: %s", name, hipGetErrorString(e));
+        return rc;
+    }
+};
+
+template <class F> void with_type(uint32_t dtype, F&& f)
+{
+    if (dtype == SLIMDP_F32) f(float{});
+    else if (dtype == SLIMDP_F16) f(_Float16{});
+    else f(__bf16{});
+}
+
+inline uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
+inline uint64_t most_rows(uint32_t n_workers, const uint64_t* rows)
+{
+    uint64_t m = 0;
+    for (uint32_t q = 0; q < n_workers; ++q) m = std::max(m, rows[q]);
+    return m;
+}
+bool shape_ok(uint32_t n_workers, const uint64_t* rows)
+{
+    return n_workers && n_workers <= SLIMDP_MAX_WORKERS && rows && most_rows(n_workers, rows) <= SLIMDP_MAX_ROWS;
+}
+
+// Rows of a slab of the sums over rows: as many slabs as give the chip eight blocks a compute unit (of 256), of sixteen rows or more.
+uint64_t slab_rows(uint64_t most, uint32_t W, uint64_t cols, size_t es)
+{
+    const uint64_t across = ceil_div(cols, 64 * (16 / es)) * W;
+    const uint64_t slabs = std::max<uint64_t>(1, std::min<uint64_t>(2048 / across, ceil_div(most, 16)));
+    return std::max<uint64_t>(1, ceil_div(most, slabs));
+}
+uint64_t column_ws(uint64_t most, uint32_t W, uint64_t cols, size_t es, int arrays)
+{
+    const uint64_t slabs = ceil_div(most, slab_rows(most, W, cols, es));
+    return slabs <= 1 ? 0 : W * slabs * arrays * cols * 4;
+}
+
+template <bool NORM> int column_grads(Call& c, ColumnArgs a, uint32_t dtype, int act, void* ws)
+{
+    constexpr int ARR = NORM ? 2 : 1;
+    a.rows = c.tab;
+    a.slab = (uint32_t)slab_rows(c.most, c.W, a.cols, c.esize);
+    a.slabs = (uint32_t)std::max<uint64_t>(1, ceil_div(c.most, a.slab));
+    a.partial = a.slabs > 1 ? static_cast<float*>(ws) : nullptr;
+    with_type(dtype, [&](auto z) {
+        typedef decltype(z) T;
+        c.launched("k_column_grads", [&] {
+            hipLaunchKernelGGL((k_column_grads<T, NORM>), dim3((uint32_t)ceil_div(a.cols, 64 * Vec<T>::N), a.slabs, c.W), dim3(256), 0,
+                               c.v.stream, a, act);
+        });
+    });
+    if (c.ok() && a.slabs > 1 && (a.out0.p[0] || a.out1.p[0] || NORM)) {
+        const ColumnSumArgs s{a.partial, a.out0, a.out1, c.tab, a.cols, a.slab, a.slabs, (uint32_t)ARR, a.accumulate};
+        c.launched("k_column_sums", [&] {
+            hipLaunchKernelGGL(k_column_sums, dim3((uint32_t)ceil_div(a.cols, 16), ARR, c.W), dim3(256), 0, c.v.stream, s);
+        });
+    }
+    return c.rc;
+}
+
+// ---------------------------------------------------------------------------------------
+// products
+// ---------------------------------------------------------------------------------------
+struct Product {
+    uint64_t M, N, K;
+    uint32_t W;
+    size_t es;
+    uint64_t tiles() const { return ceil_div(M, 128) * ceil_div(N, 128); }
+    // Few tiles leave compute units without a block: the sum is then cut, down to four steps a piece.
+    uint64_t splits() const
+    {
+        const uint64_t blocks = tiles() * W, steps = ceil_div(K, 128 / es);
+        if (blocks == 0 || blocks >= 256) return 1;
+        return std::max<uint64_t>(1, std::min({512 / blocks, steps / 4, (uint64_t)64}));
+    }
+    uint64_t piece() const { const uint64_t bk = 128 / es; return std::max<uint64_t>(1, ceil_div(ceil_div(K, bk), splits())) * bk; }
+    uint64_t ws() const { return splits() > 1 ? W * splits() * M * N * 4 : 0; }
+};
+
+template <bool AK, bool BK, int EPI> int product(Call& c, GemmArgs a, const Product& p, uint32_t dtype, void* ws)
+{
+    if (p.M == 0 || p.N == 0) return c.rc;
+    if (p.tiles() > (1u << 23)) return c.rc = host_fail(c.ctx, SLIMDP_ERR_OUT_OF_RANGE, "%s: more than 2^23 tiles of 128 x 128", c.who);
+    a.rows = c.tab;
+    a.M = (uint32_t)p.M; a.N = (uint32_t)p.N; a.K = (uint32_t)p.K;
+    a.splits = (uint32_t)p.splits();
+    a.k_split = (uint32_t)p.piece();
+    a.partial = static_cast<float*>(ws);
+    with_type(dtype, [&](auto z) {
+        typedef decltype(z) T;
+        c.launched("k_gemm", [&] {
+            hipLaunchKernelGGL((k_gemm<T, AK, BK, EPI>), dim3((uint32_t)p.tiles(), 1, c.W * a.splits), dim3(256), 0, c.v.stream, a);
+        });
+        if (c.ok() && a.splits > 1)
+            c.launched("k_gemm_join", [&] {
+                hipLaunchKernelGGL((k_gemm_join<T, EPI>), dim3((uint32_t)ceil_div(p.N, 1024), (uint32_t)std::min<uint64_t>(p.M, 1024), c.W),
+                                   dim3(256), 0, c.v.stream, a);
+            });
+    });
+    return c.rc;
+}
+
+Product forward_product(uint32_t W, uint64_t most, uint64_t in, uint64_t out, size_t es) { return {most, out, in, W, es}; }
+Product input_product(uint32_t W, uint64_t most, uint64_t in, uint64_t out, size_t es) { return {most, in, out, W, es}; }
+Product weight_product(uint32_t W, uint64_t most, uint64_t in, uint64_t out, size_t es) { return {out, in, most, W, es}; }
+
+}  // namespace
+
+extern "C" {
+
+int slimdp_layer_norm(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* rows, uint64_t cols, uint32_t dtype, const void* const* x,
+                      uint64_t ldx, const float* const* weight, const float* const* bias, float eps, void* const* y, uint64_t ldy,
+                      float* const* mean, float* const* rstd)
+{
+    Call c;
+    if (c.begin(ctx, "slimdp_layer_norm", n_workers, rows, dtype)) return c.rc;
+    c.size("cols", cols, SLIMDP_MAX_NORM_COLS);
+    c.matrix("x", x, ldx, cols, c.esize);
+    c.matrix("y", y, ldy, cols, c.esize);
+    c.params("weight", weight, 4, true);
+    c.params("bias", bias, 4, true);
+    c.matrix("mean", mean, 1, 1, 4, true);
+    c.matrix("rstd", rstd, 1, 1, 4, true);
+    c.apart("y", y, "x", x, ldx == ldy);
+    c.distinct("y", y, true);
+    c.distinct("mean", mean, true);
+    c.distinct("rstd", rstd, true);
+    if (c.ok() && !(eps > 0.0f && std::isfinite(eps))) c.rc = host_fail(ctx, SLIMDP_ERR_INVALID_ARG, "slimdp_layer_norm: eps must be positive and finite");
+    if (!c.ok() || c.most == 0) return c.rc;
+    const NormArgs a{c.in(x), c.in(weight), c.in(bias), c.out(y), c.out(mean), c.out(rstd), c.tab, ldx, ldy, (uint32_t)cols, eps};
+    with_type(dtype, [&](auto z) {
+        typedef decltype(z) T;
+        const uint64_t n = ceil_div(cols, Vec<T>::N);
+        auto launch = [&](auto kernel, uint32_t tpr) {
+            const uint32_t block = std::max(tpr, 256u), groups = block / tpr;
+            const uint64_t want = ceil_div(c.most, groups), cap = std::max<uint64_t>(1, 65536 / groups);
+            c.launched("k_norm", [&] {
+                hipLaunchKernelGGL(kernel, dim3((uint32_t)std::min(want, cap), c.W), dim3(block), 0, c.v.stream, a);
+            });
+        };
+        if (n <= 8) launch(k_norm<T, 8, 1>, 8);
+        else if (n <= 16) launch(k_norm<T, 16, 1>, 16);
+        else if (n <= 32) launch(k_norm<T, 32, 1>, 32);
+        else if (n <= 64) launch(k_norm<T, 64, 1>, 64);
+        else if (n <= 128) launch(k_norm<T, 64, 2>, 64);
+        else if (n <= 256) launch(k_norm<T, 256, 1>, 256);
+        else if (n <= 512) launch(k_norm<T, 256, 2>, 256);
+        else if (n <= 1024) launch(k_norm<T, 256, 4>, 256);
+        else if (n <= 4096) launch(k_norm<T, 1024, 4>, 1024);
+        else if (n <= 8192) launch(k_norm<T, 1024, 8>, 1024);
+        else if constexpr (Vec<T>::N == 4) launch(k_norm<T, 1024, 16>, 1024);
+    });
+    return c.rc;
+}
+
+uint64_t slimdp_layer_norm_workspace_bytes(uint32_t n_workers, const uint64_t* rows, uint64_t cols, uint32_t dtype)
+{
+    if (!shape_ok(n_workers, rows) || cols == 0 || cols > SLIMDP_MAX_NORM_COLS || dtype > SLIMDP_BF16) return 0;
+    return column_ws(most_rows(n_workers, rows), n_workers, cols, dtype == SLIMDP_F32 ? 4 : 2, 2);
+}
+
+int slimdp_layer_norm_backward(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* rows, uint64_t cols, uint32_t dtype,
+                               const void* const* dy, uint64_t lddy, const void* const* x, uint64_t ldx, const float* const* weight,
+                               const float* const* mean, const float* const* rstd, void* const* dx, uint64_t lddx,
+                               float* const* dweight, float* const* dbias, uint32_t flags, void* workspace, uint64_t workspace_bytes)
+{
+    Call c;
+    if (c.begin(ctx, "slimdp_layer_norm_backward", n_workers, rows, dtype)) return c.rc;
+    if (flags & ~SLIMDP_GRAD_ACCUMULATE)
+        return host_fail(ctx, SLIMDP_ERR_INVALID_ARG, "slimdp_layer_norm_backward: unknown flag bits 0x%x", flags);
+    const bool sums = dweight || dbias;
+    c.size("cols", cols, SLIMDP_MAX_NORM_COLS);
+    c.matrix("dy", dy, lddy, cols, c.esize);
+    c.matrix("x", x, ldx, cols, c.esize);
+    c.matrix("mean", mean, 1, 1, 4);
+    c.matrix("rstd", rstd, 1, 1, 4);
+    c.matrix("dx", dx, lddx, cols, c.esize, true);
+    c.params("weight", weight, 4, true);
+    c.params("dweight", dweight, 4, true);
+    c.params("dbias", dbias, 4, true);
+    c.apart("dx", dx, "dy", dy, lddx == lddy);
+    c.apart("dx", dx, "x", x, lddx == ldx);
+    c.distinct("dx", dx, true);
+    c.distinct("dweight", dweight, false);
+    c.distinct("dbias", dbias, false);
+    if (sums) c.workspace(workspace, workspace_bytes, slimdp_layer_norm_workspace_bytes(n_workers, rows, cols, dtype));
+    if (!c.ok()) return c.rc;
+    if (sums) {      // before dx, which may overwrite dy or x
+        ColumnArgs s{};
+        s.a = c.in(dy); s.b = c.in(x); s.mean = c.in(mean); s.rstd = c.in(rstd);
+        s.out0 = c.out(dweight); s.out1 = c.out(dbias);
+        s.lda = lddy; s.ldb = ldx; s.cols = (uint32_t)cols;
+        s.accumulate = (flags & SLIMDP_GRAD_ACCUMULATE) != 0;
+        if (column_grads<true>(c, s, dtype, ACT_NONE, workspace)) return c.rc;
+    }
+    if (!dx || c.most == 0) return c.rc;
+    const NormBackArgs a{c.in(dy), c.in(x), c.in(weight), c.in(mean), c.in(rstd), c.out(dx), c.tab, lddy, ldx, lddx, (uint32_t)cols};
+    with_type(dtype, [&](auto z) {
+        typedef decltype(z) T;
+        c.launched("k_norm_back_rows", [&] {
+            hipLaunchKernelGGL(k_norm_back_rows<T>, dim3((uint32_t)std::min<uint64_t>(c.most, 65536), c.W), dim3(256), 0, c.v.stream, a);
+        });
+    });
+    return c.rc;
+}
+
+uint64_t slimdp_linear_workspace_bytes(uint32_t n_workers, const uint64_t* rows, uint64_t in, uint64_t out, uint32_t dtype, uint32_t pass)
+{
+    if (!shape_ok(n_workers, rows) || in == 0 || in > SLIMDP_MAX_FEATURES || out == 0 || out > SLIMDP_MAX_FEATURES || dtype > SLIMDP_BF16 ||
+        pass > SLIMDP_LINEAR_BACKWARD)
+        return 0;
+    const size_t es = dtype == SLIMDP_F32 ? 4 : 2;
+    const uint64_t most = most_rows(n_workers, rows);
+    if (pass == SLIMDP_LINEAR_FORWARD) return forward_product(n_workers, most, in, out, es).ws();
+    if (pass == SLIMDP_LINEAR_EPILOGUE_BACKWARD) return column_ws(most, n_workers, out, es, 1);
+    return std::max(input_product(n_workers, most, in, out, es).ws(), weight_product(n_workers, most, in, out, es).ws());
+}
+
+int slimdp_linear(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* rows, uint64_t in, uint64_t out, uint32_t dtype,
+                  const void* const* x, uint64_t ldx, const void* const* weight, uint64_t ldw, const float* const* bias,
+                  uint32_t activation, const void* const* residual, uint64_t ldr, void* const* y, uint64_t ldy, void* const* z,
+                  uint64_t ldz, void* workspace, uint64_t workspace_bytes)
+{
+    Call c;
+    if (c.begin(ctx, "slimdp_linear", n_workers, rows, dtype)) return c.rc;
+    if (activation >= ACTS) return host_fail(ctx, SLIMDP_ERR_INVALID_ARG, "slimdp_linear: unknown activation %u", activation);
+    c.size("in", in, SLIMDP_MAX_FEATURES);
+    c.size("out", out, SLIMDP_MAX_FEATURES);
+    c.matrix("x", x, ldx, in, c.esize);
+    c.matrix("weight", weight, ldw, in, c.esize);
+    c.params("bias", bias, 4, true);
+    c.matrix("residual", residual, ldr, out, c.esize, true);
+    c.matrix("y", y, ldy, out, c.esize);
+    c.matrix("z", z, ldz, out, c.esize, true);
+    c.apart("y", y, "x", x);
+    c.apart("z", z, "x", x);
+    c.apart("y", y, "weight", weight);
+    c.apart("z", z, "weight", weight);
+    c.apart("z", z, "y", y);
+    c.apart("z", z, "residual", residual);
+    c.apart("y", y, "residual", residual, ldy == ldr);
+    c.distinct("y", y, true);
+    c.distinct("z", z, true);
+    c.workspace(workspace, workspace_bytes, slimdp_linear_workspace_bytes(n_workers, rows, in, out, dtype, SLIMDP_LINEAR_FORWARD));
+    if (!c.ok()) return c.rc;
+    GemmArgs a{};
+    a.a = c.in(x); a.b = c.in(weight); a.bias = c.in(bias); a.residual = c.in(residual);
+    a.c = c.out(y); a.z = c.out(z);
+    a.lda = ldx; a.ldb = ldw; a.ldc = ldy; a.ldr = ldr; a.ldz = ldz;
+    a.act = (int)activation;
+    return product<false, false, 0>(c, a, forward_product(c.W, c.most, in, out, c.esize), dtype, workspace);
+}
+
+int slimdp_linear_epilogue_backward(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* rows, uint64_t out, uint32_t dtype,
+                                    const void* const* dy, uint64_t lddy, const void* const* z, uint64_t ldz, uint32_t activation,
+                                    void* const* dz, uint64_t lddz, float* const* dbias, uint32_t flags, void* workspace,
+                                    uint64_t workspace_bytes)
+{
+    Call c;
+    if (c.begin(ctx, "slimdp_linear_epilogue_backward", n_workers, rows, dtype)) return c.rc;
+    if (activation >= ACTS) return host_fail(ctx, SLIMDP_ERR_INVALID_ARG, "slimdp_linear_epilogue_backward: unknown activation %u", activation);
+    if (flags & ~SLIMDP_GRAD_ACCUMULATE)
+        return host_fail(ctx, SLIMDP_ERR_INVALID_ARG, "slimdp_linear_epilogue_backward: unknown flag bits 0x%x", flags);
+    c.size("out", out, SLIMDP_MAX_FEATURES);
+    c.matrix("dy", dy, lddy, out, c.esize);
+    c.matrix("z", z, ldz, out, c.esize, activation == ACT_NONE);
+    c.matrix("dz", dz, lddz, out, c.esize, true);
+    c.params("dbias", dbias, 4, true);
+    c.apart("dz", dz, "dy", dy, lddz == lddy);
+    c.apart("dz", dz, "z", z, lddz == ldz);
+    c.distinct("dz", dz, true);
+    c.distinct("dbias", dbias, false);
+    if (dbias)
+        c.workspace(workspace, workspace_bytes, slimdp_linear_workspace_bytes(n_workers, rows, 1, out, dtype, SLIMDP_LINEAR_EPILOGUE_BACKWARD));
+    if (!c.ok() || (!dz && !dbias)) return c.rc;
+    ColumnArgs s{};
+    s.a = c.in(dy); s.b = c.in(z); s.dz = c.out(dz); s.out1 = c.out(dbias);
+    s.lda = lddy; s.ldb = ldz; s.lddz = lddz; s.cols = (uint32_t)out;
+    s.accumulate = (flags & SLIMDP_GRAD_ACCUMULATE) != 0;
+    return column_grads<false>(c, s, dtype, (int)activation, workspace);
+}
+
+int slimdp_linear_backward(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* rows, uint64_t in, uint64_t out, uint32_t dtype,
+                           const void* const* dz, uint64_t lddz, const void* const* x, uint64_t ldx, const void* const* weight,
+                           uint64_t ldw, void* const* dx, uint64_t lddx, float* const* dweight, uint32_t flags, void* workspace,
+                           uint64_t workspace_bytes)
+{
+    Call c;
+    if (c.begin(ctx, "slimdp_linear_backward", n_workers, rows, dtype)) return c.rc;
+    if (flags & ~SLIMDP_GRAD_ACCUMULATE)
+        return host_fail(ctx, SLIMDP_ERR_INVALID_ARG, "slimdp_linear_backward: unknown flag bits 0x%x", flags);
+    c.size("in", in, SLIMDP_MAX_FEATURES);
+    c.size("out", out, SLIMDP_MAX_FEATURES);
+    c.matrix("dz", dz, lddz, out, c.esize);
+    c.matrix("x", x, ldx, in, c.esize, !dweight);
+    c.matrix("weight", weight, ldw, in, c.esize, !dx);
+    c.matrix("dx", dx, lddx, in, c.esize, true);
+    c.params("dweight", dweight, 4, true);
+    c.apart("dx", dx, "dz", dz);
+    c.apart("dx", dx, "x", x);
+    c.apart("dx", dx, "weight", weight);
+    c.distinct("dx", dx, true);
+    c.distinct("dweight", dweight, false);
+    const Product pi = input_product(n_workers, c.most, in, out, c.esize), pw = weight_product(n_workers, c.most, in, out, c.esize);
+    if (c.ok() && dweight)
+        for (uint32_t q = 0; q < n_workers; ++q)
+            if (!dweight[q]) c.rc = host_fail(ctx, SLIMDP_ERR_INVALID_ARG, "slimdp_linear_backward: dweight[%u] is NULL", q);
+    c.workspace(workspace, workspace_bytes, std::max(dx ? pi.ws() : 0, dweight ? pw.ws() : 0));
+    if (!c.ok()) return c.rc;
+    if (dx) {
+        GemmArgs a{};
+        a.a = c.in(dz); a.b = c.in(weight); a.c = c.out(dx);
+        a.lda = lddz; a.ldb = ldw; a.ldc = lddx;
+        if (product<false, true, 1>(c, a, pi, dtype, workspace)) return c.rc;
+    }
+    if (dweight) {
+        GemmArgs a{};
+        a.a = c.in(dz); a.b = c.in(x); a.c = c.out(dweight);
+        a.lda = lddz; a.ldb = ldx; a.ldc = in;
+        a.k_is_rows = 1;
+        a.accumulate = (flags & SLIMDP_GRAD_ACCUMULATE) != 0;
+        product<true, true, 2>(c, a, pw, dtype, workspace);
+    }
+    return c.rc;
+}
+
+int slimdp_distill_loss(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* rows, uint64_t vocab, uint32_t dtype,
+                        const void* const* logits, uint64_t ldl, uint64_t top, const uint32_t* const* index, const float* const* value,
+                        uint64_t ldt, float temperature, const float* const* row_weight, float* const* loss, float* const* lse,
+                        void* const* dlogits, uint64_t lddl)
+{
+    Call c;
+    if (c.begin(ctx, "slimdp_distill_loss", n_workers, rows, dtype)) return c.rc;
+    c.size("vocab", vocab, SLIMDP_MAX_VOCAB);
+    if (c.ok() && top > SLIMDP_MAX_TEACHER)
+        c.rc = host_fail(ctx, SLIMDP_ERR_OUT_OF_RANGE, "slimdp_distill_loss: top exceeds %u", SLIMDP_MAX_TEACHER);
+    c.matrix("logits", logits, ldl, vocab, c.esize);
+    if (top) {
+        c.matrix("index", index, ldt, top, 4);
+        c.matrix("value", value, ldt, top, 4);
+    }
+    c.matrix("row_weight", row_weight, 1, 1, 4, true);
+    c.matrix("loss", loss, 1, 1, 4, true);
+    c.matrix("lse", lse, 1, 1, 4, true);
+    c.matrix("dlogits", dlogits, lddl, vocab, c.esize, true);
+    c.apart("dlogits", dlogits, "logits", logits, lddl == ldl);
+    c.distinct("dlogits", dlogits, true);
+    c.distinct("loss", loss, true);
+    c.distinct("lse", lse, true);
+    if (c.ok() && !(temperature > 0.0f && std::isfinite(temperature) && std::isfinite(1.0f / temperature)))
+        c.rc = host_fail(ctx, SLIMDP_ERR_INVALID_ARG, "slimdp_distill_loss: temperature must be positive and finite");
+    if (!c.ok() || c.most == 0) return c.rc;
+    const DistillArgs a{c.in(logits), c.in(top ? index : nullptr), c.in(top ? value : nullptr), c.in(row_weight), c.out(loss), c.out(lse),
+                        c.out(dlogits), c.tab, ldl, ldt, lddl, (uint32_t)vocab, (uint32_t)top, temperature, c.v.status};
+    with_type(dtype, [&](auto z) {
+        typedef decltype(z) T;
+        c.launched("k_distill", [&] {
+            hipLaunchKernelGGL(k_distill<T>, dim3((uint32_t)std::min<uint64_t>(c.most, 65536), c.W), dim3(256), 0, c.v.stream, a);
+        });
+    });
+    return c.rc;
+}
+
+}  // extern "C"
