@@ -194,6 +194,22 @@ __device__ __forceinline__ float act_value(float z, int act)
     }
 }
 
+// The same for several values: one choice for all of them.
+template <int N> __device__ __forceinline__ void act_values(float (&v)[N], int act)
+{
+    auto all = [&](auto f) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = f(v[i]);
+    };
+    switch (act) {
+    case ACT_RELU: all([](float z) { return act_value(z, ACT_RELU); }); break;
+    case ACT_GELU: all([](float z) { return act_value(z, ACT_GELU); }); break;
+    case ACT_GELU_TANH: all([](float z) { return act_value(z, ACT_GELU_TANH); }); break;
+    case ACT_SILU: all([](float z) { return act_value(z, ACT_SILU); }); break;
+    default: break;
+    }
+}
+
 // NORM: out0 = sum dy * xh, out1 = sum dy.  Otherwise dz = dy * act'(z) and out1 = sum dz, from the values before they are rounded.
 template <class T, bool NORM>
 __global__ __launch_bounds__(256) void k_column_grads(ColumnArgs a, int act)

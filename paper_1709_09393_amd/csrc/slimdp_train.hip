@@ -11,6 +11,7 @@
 #include "slimdp_host.h"
 #include "slimdp_norm.h"
 #include "slimdp_linear.h"
+#include "slimdp_gemm.h"
 #include "slimdp_distill.h"
 
 using namespace slimdp;
@@ -223,6 +224,19 @@ struct Product {
     uint64_t ws() const { return splits() > 1 ? W * splits() * M * N * 4 : 0; }
 };
 
+// Whether the tiles can be copied into the LDS as they lie: whole vectors of sixteen bytes on their own alignment, and
+// distances that fit the copies' offsets.
+template <bool AK, bool BK> bool by_copies(const Call& c, const GemmArgs& a, const Product& p)
+{
+    auto fits = [&](const InTab& t, uint64_t ld, uint64_t run) {
+        if (ld % 8 || run % 8 || ld > (1u << 21)) return false;
+        for (uint32_t q = 0; q < c.W; ++q)
+            if (reinterpret_cast<uintptr_t>(t.p[q]) % 16) return false;
+        return true;
+    };
+    return fits(a.a, a.lda, AK ? p.M : p.K) && fits(a.b, a.ldb, BK ? p.N : p.K) && p.splits() == 1 && p.M > 128 && p.N > 128;
+}
+
 template <bool AK, bool BK, int EPI> int product(Call& c, GemmArgs a, const Product& p, uint32_t dtype, void* ws)
 {
     if (p.M == 0 || p.N == 0) return c.rc;
@@ -232,6 +246,16 @@ template <bool AK, bool BK, int EPI> int product(Call& c, GemmArgs a, const Prod
     a.splits = (uint32_t)p.splits();
     a.k_split = (uint32_t)p.piece();
     a.partial = static_cast<float*>(ws);
+    if (dtype != SLIMDP_F32 && by_copies<AK, BK>(c, a, p)) {
+        auto launch = [&](auto z) {
+            typedef decltype(z) T;
+            c.launched("k_gemm_tiles", [&] {
+                hipLaunchKernelGGL((k_gemm_tiles<T, AK, BK, EPI, 256, 256, 2, 2>), dim3((uint32_t)(ceil_div(p.M, 256) * ceil_div(p.N, 256)), 1, c.W * a.splits), dim3(256), 0, c.v.stream, a);
+            });
+        };
+        if (dtype == SLIMDP_F16) launch(_Float16{}); else launch(__bf16{});
+        return c.rc;
+    }
     with_type(dtype, [&](auto z) {
         typedef decltype(z) T;
         c.launched("k_gemm", [&] {
