@@ -1,5 +1,6 @@
 // Distillation from a teacher's top logits: loss of every row and gradient of the student's logits.  Included only by slimdp_train.hip.
 #pragma once
+#include "slimdp_host.h"
 #include "slimdp_train.h"
 
 namespace slimdp {
@@ -18,119 +19,224 @@ struct DistillArgs {
 
 // Per row, with s = logits / tau over the vocabulary, q = softmax(s), v = value / tau of the row's valid entries and p = softmax(v):
 //     lse = log sum exp(s),   loss = w tau^2 sum_j p_j (log p_j - (s[index_j] - lse)),   dlogits = w tau (q - sum over j at v of p_j)
-// One block of 256 threads a row; the logits are read twice, the second time from the caches.
-// An entry that appears twice counts twice; the first of equal indices carries the sum of all, so that one thread
-// writes each place and the sum's order is that of the list.
-template <class T>
-__global__ __launch_bounds__(256) void k_distill(DistillArgs a)
+//
+// One block of BT threads a row, which takes MINE of the teacher's entries a thread.  HELD > 0: the row stays in registers, HELD vectors of sixteen bytes a thread, so that it is read
+// once and written once; the sum's exponentials are taken as the vectors arrive (against each thread's own largest value so far),
+// the gradient's as they leave, and neither waits for the other's memory.  HELD = 0: rows that no block holds, read twice, and calls that ask for no
+// gradient (nothing is kept then: 128,000 columns of bf16, 4,096 rows: 192 us instead of 294).  NT: streams pass the caches by.
+// Exponentials are powers of two of (x - largest) * (log2 e / tau): the difference first, so that logits far from zero (a mask of the
+// type's lowest value over a whole row among them) lose nothing to the product's rounding.
+//
+// The teacher's entries are subtracted by the threads that own their places: every thread has a list of the entries in its vectors.
+// An entry that appears twice counts twice: the first of equal indices carries the sum, added in the order of the entries, and
+// the others nothing, so that no order of threads shows in the result.
+template <class T, int BT, int HELD, int MINE, int NT>
+__global__ __launch_bounds__(BT) void k_distill(DistillArgs a)
 {
-    constexpr int V = Vec<T>::N, BT = 256;
-    __shared__ float tp[TEACHER_MAX];
-    __shared__ uint32_t ti[TEACHER_MAX];
-    __shared__ float slots[6][BT / 64];
-    const uint32_t q = blockIdx.y, rows = a.rows.n[q], vocab = a.vocab, top = a.top, t = threadIdx.x;
+    constexpr int V = Vec<T>::N, WAVES = BT / 64, ROOM = BT * MINE;
+    constexpr float LOG2E = 1.4426950408889634f;
+    __shared__ float tp[ROOM];                       // p of every entry; then what its place loses
+    __shared__ uint32_t ti[ROOM];
+    __shared__ uint16_t follow[ROOM];
+    __shared__ uint32_t head[BT];
+    __shared__ uint32_t held_slots[BT];              // bit: the list has an entry in vector (number mod 32) of the thread
+    __shared__ float slots[5][WAVES];
+    const uint32_t q = blockIdx.y, rows = a.rows.n[q], vocab = a.vocab, top = a.top, t = threadIdx.x, wave = t >> 6;
     const T* logits = static_cast<const T*>(a.logits.p[q]);
     const uint32_t* index = static_cast<const uint32_t*>(a.index.p[q]);
     const float* value = static_cast<const float*>(a.value.p[q]);
     const float* row_weight = static_cast<const float*>(a.row_weight.p[q]);
     T* dlogits = static_cast<T*>(a.dlogits.p[q]);
-    const float inv_tau = 1.0f / a.tau;
-    auto block_max = [&](float v, float* s) {
-        v = wave_max_f(v);
-        if ((t & 63u) == 0) s[t >> 6] = v;
-        __syncthreads();
-        return fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+    const float inv_tau = 1.0f / a.tau, scale2 = inv_tau * LOG2E;
+    const float INF = __builtin_inff();
+    auto put = [&](float v, float* s) { if ((t & 63u) == 0) s[wave] = v; };
+    auto sum_of = [&](const float* s) {
+        float v = s[0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) v += s[w];
+        return v;
+    };
+    auto max_of = [&](const float* s) {
+        float v = s[0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) v = fmaxf(v, s[w]);
+        return v;
     };
     for (uint32_t r = blockIdx.x; r < rows; r += gridDim.x) {
         const T* row = logits + (size_t)r * a.ldl;
+        raw4 x[HELD ? HELD : 1];
+        if constexpr (HELD > 0) {
+#pragma unroll
+            for (int j = 0; j < HELD; ++j) {
+                const uint32_t c = ((uint32_t)j * BT + t) * V;
+                if (c < vocab) x[j] = load_clip<T, NT>(row, c, vocab);
+            }
+        }
         const float w = row_weight ? row_weight[r] : 1.0f;
-        // the teacher's distribution
-        float vmax = -__builtin_inff();
-        for (uint32_t j = t; j < top; j += BT) {
-            uint32_t i = index[(size_t)r * a.ldt + j];
-            float v = -__builtin_inff();
-            if (i < vocab) v = value[(size_t)r * a.ldt + j] * inv_tau;
-            else {
-                if (i != 0xFFFFFFFFu) atomicOr(a.status, 4u);
-                i = 0xFFFFFFFFu;
+        // the teacher's distribution, and the student's logits at its entries
+        float vmax = -INF, logit[MINE], mine[MINE];
+        uint32_t at[MINE];
+        head[t] = 0xFFFFu;
+        held_slots[t] = 0;
+#pragma unroll
+        for (int k = 0; k < MINE; ++k) {
+            const uint32_t j = k * BT + t;
+            at[k] = 0xFFFFFFFFu;
+            mine[k] = -INF;
+            logit[k] = 0.0f;
+            if (j >= top) continue;
+            at[k] = index[(size_t)r * a.ldt + j];
+            if (at[k] < vocab) {
+                mine[k] = value[(size_t)r * a.ldt + j] * inv_tau;
+                logit[k] = (float)row[at[k]];
+            } else {
+                if (at[k] != 0xFFFFFFFFu) atomicOr(a.status, STATUS_TEACHER);
+                at[k] = 0xFFFFFFFFu;
             }
-            ti[j] = i;
-            tp[j] = v;
-            vmax = fmaxf(vmax, v);
+            vmax = fmaxf(vmax, mine[k]);
         }
-        vmax = block_max(vmax, slots[0]);
-        const bool some = vmax != -__builtin_inff();
+        put(wave_max_f(vmax), slots[0]);
+        __syncthreads();
+        vmax = max_of(slots[0]);
+        const bool live = vmax != -INF && w != 0.0f;
         float mass = 0.0f;
-        if (some)
-            for (uint32_t j = t; j < top; j += BT)
-                if (ti[j] != 0xFFFFFFFFu) mass += expf(tp[j] - vmax);
-        mass = group_sum<BT>(mass, slots[1]);
+#pragma unroll
+        for (int k = 0; k < MINE; ++k)
+            if (live && at[k] != 0xFFFFFFFFu) mass += expf(mine[k] - vmax);
+        put(wave_sum_f(mass), slots[1]);
+        __syncthreads();
+        const float log_mass = logf(sum_of(slots[1]));
+#pragma unroll
+        for (int k = 0; k < MINE; ++k) {
+            const uint32_t j = k * BT + t;
+            if (j >= top) continue;
+            mine[k] = live ? mine[k] - vmax - log_mass : -INF;                 // log p
+            ti[j] = at[k];
+            tp[j] = at[k] != 0xFFFFFFFFu ? expf(mine[k]) : 0.0f;
+            if (live && dlogits && at[k] != 0xFFFFFFFFu) {
+                const uint32_t vec = at[k] / V, owner = vec % BT;
+                follow[j] = (uint16_t)atomicExch(&head[owner], j);
+                atomicOr(&held_slots[owner], 1u << (vec / BT & 31u));
+            }
+        }
         // the student's largest logit and sum of exponentials
-        float top_s = -__builtin_inff();
-        for (uint32_t c = t * V; c < vocab; c += BT * V) {
-            float f[V];
-            unpack<T>(load_clip(row, c, vocab), f);
+        float m = -INF, sum = 0.0f;
+        auto take = [&](raw4 v, uint32_t c) {
+            float f[V], big = -INF;
+            unpack<T>(v, f);
+            if (c + V > vocab)
 #pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (c + i < vocab) top_s = fmaxf(top_s, f[i]);
-        }
-        top_s = block_max(top_s, slots[2]) * inv_tau;
-        if (top_s == -__builtin_inff()) top_s = 0.0f;
-        float sum = 0.0f;
-        for (uint32_t c = t * V; c < vocab; c += BT * V) {
-            float f[V];
-            unpack<T>(load_clip(row, c, vocab), f);
+                for (int i = 0; i < V; ++i)
+                    if (c + i >= vocab) f[i] = -INF;
 #pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (c + i < vocab) sum += expf(f[i] * inv_tau - top_s);
+            for (int i = 0; i < V; ++i) big = fmaxf(big, f[i]);
+            if (big > m) {
+                sum *= __builtin_amdgcn_exp2f((m - big) * scale2);             // the first time: 0 * 0
+                m = big;
+            }
+            const float ref = m == -INF ? 0.0f : m;
+#pragma unroll
+            for (int i = 0; i < V; ++i) sum += __builtin_amdgcn_exp2f((f[i] - ref) * scale2);
+        };
+        if constexpr (HELD > 0) {
+#pragma unroll
+            for (int j = 0; j < HELD; ++j) {
+                const uint32_t c = ((uint32_t)j * BT + t) * V;
+                if (c < vocab) take(x[j], c);
+            }
+        } else {
+            for (uint32_t c = t * V; c < vocab; c += BT * V) take(load_clip(row, c, vocab), c);
         }
-        sum = group_sum<BT>(sum, slots[3]);
-        const float lse = top_s + logf(sum), log_mass = logf(mass);
+        const float wave_m = wave_max_f(m);
+        sum = m == -INF ? sum : sum * __builtin_amdgcn_exp2f((m - wave_m) * scale2);      // nothing but -inf seen: 0, or NaN
+        put(wave_m, slots[2]);
+        put(wave_sum_f(sum), slots[3]);
+        __syncthreads();
+        m = max_of(slots[2]);
+        if (m == -INF) m = 0.0f;
+        sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) {
+            const float wm = slots[2][i], ws = slots[3][i];
+            sum += wm == -INF ? ws : ws * __builtin_amdgcn_exp2f((wm - m) * scale2);
+        }
+        const float log_sum = logf(sum), lse = m * inv_tau + log_sum;
         float loss = 0.0f;
-        if (some && w != 0.0f)
-            for (uint32_t j = t; j < top; j += BT) {
-                if (ti[j] == 0xFFFFFFFFu) continue;
-                const float l = tp[j] - vmax - log_mass, p = expf(l);
-                if (p != 0.0f) loss += p * (l - ((float)row[ti[j]] * inv_tau - lse));
-            }
-        loss = group_sum<BT>(loss, slots[4]);
-        if (t == 0) {
-            if (a.loss.p[q]) static_cast<float*>(a.loss.p[q])[r] = some && w != 0.0f ? w * a.tau * a.tau * loss : 0.0f;
-            if (a.lse.p[q]) static_cast<float*>(a.lse.p[q])[r] = lse;
+#pragma unroll
+        for (int k = 0; k < MINE; ++k) {
+            const uint32_t j = k * BT + t;
+            if (!live || j >= top || at[k] == 0xFFFFFFFFu) continue;
+            const float p = tp[j];
+            if (p != 0.0f) loss += p * (mine[k] - ((logit[k] - m) * inv_tau - log_sum));
         }
-        if (dlogits) {
-            T* out = dlogits + (size_t)r * a.lddl;
-            const float scale = w * a.tau;
-            const bool live = some && w != 0.0f;
-            // each entry's final value, taken before the row may be overwritten (dlogits may be logits)
-            float mine[(TEACHER_MAX + BT - 1) / BT];
+        put(wave_sum_f(loss), slots[4]);
+        // equal indices: whoever finds another one in the list of their place
+        float lost[MINE];
 #pragma unroll
-            for (int k = 0; k < (TEACHER_MAX + BT - 1) / BT; ++k) {
-                const uint32_t j = k * BT + t;
-                mine[k] = 0.0f;
-                if (!live || j >= top || ti[j] == 0xFFFFFFFFu) continue;
-                float p = 0.0f;
-                for (uint32_t o = 0; o < top; ++o)
-                    if (ti[o] == ti[j]) p += expf(tp[o] - vmax - log_mass);
-                mine[k] = scale * (expf((float)row[ti[j]] * inv_tau - lse) - p);
-            }
-            __syncthreads();
-            for (uint32_t c = t * V; c < vocab; c += BT * V) {
-                float f[V];
-                unpack<T>(load_clip(row, c, vocab), f);
-#pragma unroll
-                for (int i = 0; i < V; ++i) f[i] = live ? scale * expf(f[i] * inv_tau - lse) : 0.0f;
-                store_clip(out, c, vocab, pack<T>(f));
-            }
-            __syncthreads();
-            if (live)
-#pragma unroll
-                for (int k = 0; k < (TEACHER_MAX + BT - 1) / BT; ++k) {
-                    const uint32_t j = k * BT + t;
-                    if (j < top && ti[j] != 0xFFFFFFFFu) out[ti[j]] = (T)mine[k];      // equal indices: the same value
+        for (int k = 0; k < MINE; ++k) {
+            const uint32_t j = k * BT + t;
+            lost[k] = 0.0f;
+            if (!live || !dlogits || j >= top || at[k] == 0xFFFFFFFFu) continue;
+            uint32_t same = 0, before = 0;
+            for (uint32_t e = head[at[k] / V % BT]; e != 0xFFFFu; e = follow[e])
+                if (ti[e] == at[k]) {
+                    ++same;
+                    before += e < j;
                 }
+            lost[k] = before ? 0.0f : tp[j];
+            if (before || same == 1) continue;
+            if (same <= 8) {                         // the next larger one of the list, again and again
+                uint32_t last = j;
+                for (uint32_t i = 1; i < same; ++i) {
+                    uint32_t least = 0xFFFFu;
+                    for (uint32_t e = head[at[k] / V % BT]; e != 0xFFFFu; e = follow[e])
+                        if (ti[e] == at[k] && e > last && e < least) least = e;
+                    lost[k] += tp[least];
+                    last = least;
+                }
+            } else
+                for (uint32_t e = j + 1; e < top; ++e)
+                    if (ti[e] == at[k]) lost[k] += tp[e];
         }
         __syncthreads();
+        if (t == 0) {
+            if (a.loss.p[q]) static_cast<float*>(a.loss.p[q])[r] = live ? w * a.tau * a.tau * sum_of(slots[4]) : 0.0f;
+            if (a.lse.p[q]) static_cast<float*>(a.lse.p[q])[r] = lse;
+        }
+        if (!dlogits) continue;
+#pragma unroll
+        for (int k = 0; k < MINE; ++k)
+            if (live && k * BT + t < top) tp[k * BT + t] = w * a.tau * lost[k];
+        __syncthreads();
+        T* out = dlogits + (size_t)r * a.lddl;
+        const float scale = w * a.tau / sum;
+        const uint32_t touched = held_slots[t], list = head[t];
+        auto give = [&](raw4 v, uint32_t c, uint32_t j) {
+            float f[V];
+            unpack<T>(v, f);
+#pragma unroll
+            for (int i = 0; i < V; ++i) f[i] = scale * __builtin_amdgcn_exp2f((f[i] - m) * scale2);
+            if (touched >> (j & 31u) & 1u)
+                for (uint32_t e = list; e != 0xFFFFu; e = follow[e]) {
+                    const uint32_t o = ti[e] - c;
+                    const float p = tp[e];
+#pragma unroll
+                    for (int i = 0; i < V; ++i)
+                        if (o == (uint32_t)i) f[i] -= p;
+                }
+            store_clip<T, NT>(out, c, vocab, live ? pack<T>(f) : raw4{0, 0, 0, 0});
+        };
+        if constexpr (HELD > 0) {
+#pragma unroll
+            for (int j = 0; j < HELD; ++j) {
+                const uint32_t c = ((uint32_t)j * BT + t) * V;
+                if (c < vocab) give(x[j], c, j);
+            }
+        } else {
+            uint32_t j = 0;
+            for (uint32_t c = t * V; c < vocab; c += BT * V, ++j) give(load_clip(row, c, vocab), c, j);
+        }
+        __syncthreads();                             // lists and sums are written anew for the next row
     }
 }
 

@@ -522,11 +522,37 @@ int slimdp_distill_loss(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* row
     if (!c.ok() || c.most == 0) return c.rc;
     const DistillArgs a{c.in(logits), c.in(top ? index : nullptr), c.in(top ? value : nullptr), c.in(row_weight), c.out(loss), c.out(lse),
                         c.out(dlogits), c.tab, ldl, ldt, lddl, (uint32_t)vocab, (uint32_t)top, temperature, c.v.status};
+    uint64_t rows_bytes = 0;
+    for (uint32_t q = 0; q < c.W; ++q) rows_bytes += 2 * rows[q] * vocab * c.esize;
     with_type(dtype, [&](auto z) {
         typedef decltype(z) T;
-        c.launched("k_distill", [&] {
-            hipLaunchKernelGGL(k_distill<T>, dim3((uint32_t)std::min<uint64_t>(c.most, 65536), c.W), dim3(256), 0, c.v.stream, a);
-        });
+        const uint64_t n = ceil_div(vocab, Vec<T>::N);
+        auto launch = [&](auto kernel, uint32_t block) {
+            c.launched("k_distill", [&] {
+                hipLaunchKernelGGL(kernel, dim3((uint32_t)std::min<uint64_t>(c.most, 65536), c.W), dim3(block), 0, c.v.stream, a);
+            });
+        };
+        // the smallest block that holds the row, without a second entry for any thread where the lists are short.  Logits and gradients
+        // pass the caches by where they do not fit them: 4 x 1024 rows of 128,000 bf16 (2.1 GB) 533 -> 496 us with stores, 552 without
+        // loads that do; but 8 x 4096 rows of 1,000 (131 MB) 62 -> 70.
+        const bool nt = rows_bytes > (256ull << 20);
+#define SLIMDP_DISTILL_NT(BT, HELD, MINE)                                                         \
+    do { if (nt) launch(k_distill<T, BT, HELD, MINE, 1>, BT); else launch(k_distill<T, BT, HELD, MINE, 0>, BT); } while (0)
+#define SLIMDP_DISTILL(BT, HELD)                                                                  \
+    do {                                                                                          \
+        if (top <= BT) SLIMDP_DISTILL_NT(BT, HELD, 1);                                            \
+        else SLIMDP_DISTILL_NT(BT, HELD, (int)(SLIMDP_MAX_TEACHER + BT - 1) / BT);                \
+    } while (0)
+        if (!dlogits && n <= 2048) SLIMDP_DISTILL(256, 0);
+        else if (!dlogits || n > 16384) SLIMDP_DISTILL(512, 0);
+        else if (n <= 512) SLIMDP_DISTILL(128, 4);
+        else if (n <= 1024) SLIMDP_DISTILL(256, 4);
+        else if (n <= 2048) SLIMDP_DISTILL(256, 8);
+        else if (n <= 4096) SLIMDP_DISTILL(512, 8);
+        else if (n <= 8192) SLIMDP_DISTILL(512, 16);
+        else SLIMDP_DISTILL_NT(1024, 16, 1);
+#undef SLIMDP_DISTILL
+#undef SLIMDP_DISTILL_NT
     });
     return c.rc;
 }

@@ -439,11 +439,13 @@ def distill_reference(logits, index, value, tau, weight, dtype):
     logp = torch.log_softmax(v, 1)
     p = torch.where(valid & some[:, None], logp.exp(), torch.zeros_like(v))
     at = torch.where(valid, index, torch.zeros_like(index)).long()
-    logq = s.gather(1, at) - lse[:, None]
+    # from the row's largest logit, not from lse: where all logits are the type's lowest value, lse in 64 bits loses log V beside them
+    logq_all = torch.log_softmax(s, 1)
+    logq = logq_all.gather(1, at)
     diff = torch.where(p > 0, logp - logq, torch.zeros_like(p))
     w = torch.where(some, weight.double(), torch.zeros_like(weight, dtype=torch.float64))
     loss = w * tau * tau * torch.where(p > 0, p * diff, torch.zeros_like(p)).sum(1)
-    q = torch.where(some[:, None], (s - lse[:, None]).exp(), torch.zeros_like(s))
+    q = torch.where(some[:, None], logq_all.exp(), torch.zeros_like(s))
     dense = torch.zeros_like(s).scatter_add_(1, at, p)
     # errors: a scaled logit is off by two roundings of its size, an exponential by that and a few more; sums of positive terms by their depth
     fin = lambda a: torch.where(a.isfinite(), a.abs(), torch.zeros_like(a)).amax(1)
