@@ -1,5 +1,6 @@
 // Distillation from a teacher's top logits: loss of every row and gradient of the student's logits.  Included only by slimdp_train.hip.
 #pragma once
+#include "slimdp_act.h"
 #include "slimdp_host.h"
 #include "slimdp_train.h"
 
@@ -34,7 +35,6 @@ template <class T, int BT, int HELD, int MINE, int NT>
 __global__ __launch_bounds__(BT) void k_distill(DistillArgs a)
 {
     constexpr int V = Vec<T>::N, WAVES = BT / 64, ROOM = BT * MINE;
-    constexpr float LOG2E = 1.4426950408889634f;
     __shared__ float tp[ROOM];                       // p of every entry; then what its place loses
     __shared__ uint32_t ti[ROOM];
     __shared__ uint16_t follow[ROOM];
@@ -49,6 +49,10 @@ __global__ __launch_bounds__(BT) void k_distill(DistillArgs a)
     T* dlogits = static_cast<T*>(a.dlogits.p[q]);
     const float inv_tau = 1.0f / a.tau, scale2 = inv_tau * LOG2E;
     const float INF = __builtin_inff();
+    // whole vectors, and behind the last of them one element a thread
+    const uint32_t main = vocab / V * V, last = main + t;
+    const bool has_last = last < vocab;
+    auto owner_of = [&](uint32_t i) { return i < main ? i / V % BT : i - main; };
     auto put = [&](float v, float* s) { if ((t & 63u) == 0) s[wave] = v; };
     auto sum_of = [&](const float* s) {
         float v = s[0];
@@ -69,9 +73,10 @@ __global__ __launch_bounds__(BT) void k_distill(DistillArgs a)
 #pragma unroll
             for (int j = 0; j < HELD; ++j) {
                 const uint32_t c = ((uint32_t)j * BT + t) * V;
-                if (c < vocab) x[j] = load_clip<T, NT>(row, c, vocab);
+                if (c < main) x[j] = load_raw<T, NT>(row + c);
             }
         }
+        const float x_last = has_last ? (float)row[last] : 0.0f;
         const float w = row_weight ? row_weight[r] : 1.0f;
         // the teacher's distribution, and the student's logits at its entries
         float vmax = -INF, logit[MINE], mine[MINE];
@@ -114,20 +119,16 @@ __global__ __launch_bounds__(BT) void k_distill(DistillArgs a)
             ti[j] = at[k];
             tp[j] = at[k] != 0xFFFFFFFFu ? expf(mine[k]) : 0.0f;
             if (live && dlogits && at[k] != 0xFFFFFFFFu) {
-                const uint32_t vec = at[k] / V, owner = vec % BT;
+                const uint32_t owner = owner_of(at[k]);
                 follow[j] = (uint16_t)atomicExch(&head[owner], j);
-                atomicOr(&held_slots[owner], 1u << (vec / BT & 31u));
+                if (at[k] < main) atomicOr(&held_slots[owner], 1u << (at[k] / (V * BT) & 31u));
             }
         }
         // the student's largest logit and sum of exponentials
         float m = -INF, sum = 0.0f;
-        auto take = [&](raw4 v, uint32_t c) {
+        auto take = [&](raw4 v) {
             float f[V], big = -INF;
             unpack<T>(v, f);
-            if (c + V > vocab)
-#pragma unroll
-                for (int i = 0; i < V; ++i)
-                    if (c + i >= vocab) f[i] = -INF;
 #pragma unroll
             for (int i = 0; i < V; ++i) big = fmaxf(big, f[i]);
             if (big > m) {
@@ -138,14 +139,16 @@ __global__ __launch_bounds__(BT) void k_distill(DistillArgs a)
 #pragma unroll
             for (int i = 0; i < V; ++i) sum += __builtin_amdgcn_exp2f((f[i] - ref) * scale2);
         };
+        if (has_last) {
+            m = fmaxf(x_last, -INF);
+            sum = __builtin_amdgcn_exp2f((x_last - (m == -INF ? 0.0f : m)) * scale2);
+        }
         if constexpr (HELD > 0) {
 #pragma unroll
-            for (int j = 0; j < HELD; ++j) {
-                const uint32_t c = ((uint32_t)j * BT + t) * V;
-                if (c < vocab) take(x[j], c);
-            }
+            for (int j = 0; j < HELD; ++j)
+                if (((uint32_t)j * BT + t) * V < main) take(x[j]);
         } else {
-            for (uint32_t c = t * V; c < vocab; c += BT * V) take(load_clip(row, c, vocab), c);
+            for (uint32_t c = t * V; c < main; c += BT * V) take(load_raw<T>(row + c));
         }
         const float wave_m = wave_max_f(m);
         sum = m == -INF ? sum : sum * __builtin_amdgcn_exp2f((m - wave_m) * scale2);      // nothing but -inf seen: 0, or NaN
@@ -178,7 +181,7 @@ __global__ __launch_bounds__(BT) void k_distill(DistillArgs a)
             lost[k] = 0.0f;
             if (!live || !dlogits || j >= top || at[k] == 0xFFFFFFFFu) continue;
             uint32_t same = 0, before = 0;
-            for (uint32_t e = head[at[k] / V % BT]; e != 0xFFFFu; e = follow[e])
+            for (uint32_t e = head[owner_of(at[k])]; e != 0xFFFFu; e = follow[e])
                 if (ti[e] == at[k]) {
                     ++same;
                     before += e < j;
@@ -189,7 +192,7 @@ __global__ __launch_bounds__(BT) void k_distill(DistillArgs a)
                 uint32_t last = j;
                 for (uint32_t i = 1; i < same; ++i) {
                     uint32_t least = 0xFFFFu;
-                    for (uint32_t e = head[at[k] / V % BT]; e != 0xFFFFu; e = follow[e])
+                    for (uint32_t e = head[owner_of(at[k])]; e != 0xFFFFu; e = follow[e])
                         if (ti[e] == at[k] && e > last && e < least) least = e;
                     lost[k] += tp[least];
                     last = least;
@@ -224,17 +227,23 @@ __global__ __launch_bounds__(BT) void k_distill(DistillArgs a)
                     for (int i = 0; i < V; ++i)
                         if (o == (uint32_t)i) f[i] -= p;
                 }
-            store_clip<T, NT>(out, c, vocab, live ? pack<T>(f) : raw4{0, 0, 0, 0});
+            store_raw<T, NT>(out + c, live ? pack<T>(f) : raw4{0, 0, 0, 0});
         };
         if constexpr (HELD > 0) {
 #pragma unroll
             for (int j = 0; j < HELD; ++j) {
                 const uint32_t c = ((uint32_t)j * BT + t) * V;
-                if (c < vocab) give(x[j], c, j);
+                if (c < main) give(x[j], c, j);
             }
         } else {
             uint32_t j = 0;
-            for (uint32_t c = t * V; c < vocab; c += BT * V, ++j) give(load_clip(row, c, vocab), c, j);
+            for (uint32_t c = t * V; c < main; c += BT * V, ++j) give(load_raw<T>(row + c), c, j);
+        }
+        if (has_last) {
+            float f = scale * __builtin_amdgcn_exp2f((x_last - m) * scale2);
+            for (uint32_t e = list; e != 0xFFFFu; e = follow[e])
+                if (ti[e] == last) f -= tp[e];
+            out[last] = live ? (T)f : (T)0.0f;
         }
         __syncthreads();                             // lists and sums are written anew for the next row
     }

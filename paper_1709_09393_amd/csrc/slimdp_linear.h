@@ -93,7 +93,11 @@ __device__ __forceinline__ void epilogue4(const GemmArgs& a, uint32_t q, uint32_
                 if (!full && n + i >= N) break;
                 if (bias) v[i] += bias[n + i];
                 if (z) z[(size_t)m * a.ldz + n + i] = (T)v[i];
-                v[i] = act_value(v[i], a.act);
+            }
+            act_values(v, a.act);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (!full && n + i >= N) break;
                 if (res) v[i] += (float)res[(size_t)m * a.ldr + n + i];
             }
         }

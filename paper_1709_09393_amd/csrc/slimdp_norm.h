@@ -1,6 +1,7 @@
 // Layer norm of every worker's rows and its backward pass; gradient of the product's epilogue; the sums over rows that all
 // parameter vectors' gradients are.  Included only by slimdp_train.hip.
 #pragma once
+#include "slimdp_act.h"
 #include "slimdp_train.h"
 
 namespace slimdp {
@@ -16,15 +17,17 @@ struct NormArgs {
 
 // y = (x - mean) * rstd * weight + bias, mean and rstd = 1 / sqrt(var + eps) over the row, var the mean of (x - mean)^2.
 // TPR threads hold a row in registers, NC vectors of sixteen bytes each: the row is read once, and the variance is the sum of
-// squared distances from the finished mean (no cancellation, whatever the mean).  All sums in binary32.
+// squared distances from the finished mean (no cancellation, whatever the mean).  All sums in binary32.  Bound by memory: a block takes
+// several rows and asks for the next one before it sums the present one; weight and bias stay in registers where they are few (KEEP).
 // grid (blocks, workers); groups of TPR threads take rows in turn.
-template <class T, int TPR, int NC>
+template <class T, int TPR, int NC, int NT>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_norm(NormArgs a)
 {
     constexpr int BT = TPR > 256 ? TPR : 256, GROUPS = BT / TPR, V = Vec<T>::N;
+    constexpr bool KEEP = NC * V <= 16, AHEAD = NC < 8;
     __shared__ float slots[2][BT / 64];
     const uint32_t q = blockIdx.y, rows = a.rows.n[q], cols = a.cols;
-    const uint32_t lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
+    const uint32_t lane = threadIdx.x % TPR, group = threadIdx.x / TPR, step = gridDim.x * GROUPS;
     const T* x = static_cast<const T*>(a.x.p[q]);
     T* y = static_cast<T*>(a.y.p[q]);
     const float* weight = static_cast<const float*>(a.weight.p[q]);
@@ -32,29 +35,65 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_norm(NormArgs a)
     float* mean_out = static_cast<float*>(a.mean.p[q]);
     float* rstd_out = static_cast<float*>(a.rstd.p[q]);
     const float count = (float)cols;
-    for (uint32_t r = blockIdx.x * GROUPS + group; r < rows; r += gridDim.x * GROUPS) {
+    // whole vectors, and behind the last of them one element a lane
+    const uint32_t main = cols / V * V, last = main + lane;
+    const bool has_last = last < cols;
+    auto column = [&](int j) { return ((uint32_t)j * TPR + lane) * V; };
+    auto params = [&](int j, float (&g)[V], float (&b)[V]) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) { g[i] = 1.0f; b[i] = 0.0f; }
+        if (weight) load_whole<V>(weight + column(j), g);
+        if (bias) load_whole<V>(bias + column(j), b);
+    };
+    float kg[KEEP ? NC : 1][V], kb[KEEP ? NC : 1][V];
+    if constexpr (KEEP)
+#pragma unroll
+        for (int j = 0; j < NC; ++j)
+            if (column(j) < main) params(j, kg[j], kb[j]);
+    const float last_g = has_last && weight ? weight[last] : 1.0f, last_b = has_last && bias ? bias[last] : 0.0f;
+    raw4 now[NC], next[AHEAD ? NC : 1];
+    float now_last = 0.0f, next_last = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NC; ++j) now[j] = raw4{0, 0, 0, 0};          // columns behind the row's end stay zero
+    if constexpr (AHEAD)
+#pragma unroll
+        for (int j = 0; j < NC; ++j) next[j] = raw4{0, 0, 0, 0};
+    auto load_row = [&](uint32_t r, auto& v, float& l) {
+        if (r >= rows) return;
         const T* xr = x + (size_t)r * a.ldx;
-        float f[NC][V], s = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NC; ++j)
+            if (column(j) < main) v[j] = load_raw<T, NT>(xr + column(j));
+        if (has_last) l = (float)xr[last];
+    };
+    uint32_t r = blockIdx.x * GROUPS + group;
+    if constexpr (AHEAD) load_row(r, next, next_last);
+    for (; r < rows; r += step) {
+        if constexpr (AHEAD) {
+#pragma unroll
+            for (int j = 0; j < NC; ++j) now[j] = next[j];
+            now_last = next_last;
+            load_row(r + step, next, next_last);
+        } else load_row(r, now, now_last);
+        float s = now_last;
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
-            const uint32_t c = ((uint32_t)j * TPR + lane) * V;
-            if (c < cols) unpack<T>(load_clip(xr, c, cols), f[j]);
-            else {
+            float f[V];
+            unpack<T>(now[j], f);
 #pragma unroll
-                for (int i = 0; i < V; ++i) f[j][i] = 0.0f;
-            }
-#pragma unroll
-            for (int i = 0; i < V; ++i) s += f[j][i];
+            for (int i = 0; i < V; ++i) s += f[i];
         }
         const float mean = group_sum<TPR>(s, slots[0]) / count;
-        s = 0.0f;
+        s = has_last ? (now_last - mean) * (now_last - mean) : 0.0f;
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
-            const uint32_t c = ((uint32_t)j * TPR + lane) * V;
+            if (column(j) >= main) continue;
+            float f[V];
+            unpack<T>(now[j], f);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                f[j][i] = c + i < cols ? f[j][i] - mean : 0.0f;
-                s = __builtin_fmaf(f[j][i], f[j][i], s);
+                const float d = f[i] - mean;
+                s = __builtin_fmaf(d, d, s);
             }
         }
         const float var = group_sum<TPR>(s, slots[1]) / count;
@@ -66,21 +105,19 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void k_norm(NormArgs a)
         T* yr = y + (size_t)r * a.ldy;
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
-            const uint32_t c = ((uint32_t)j * TPR + lane) * V;
-            if (c < cols) {
-                float g[V], b[V];
-                if (weight) load_params<V>(weight, c, cols, g);
-                if (bias) load_params<V>(bias, c, cols, b);
+            if (column(j) >= main) continue;
+            float f[V], g[V], b[V];
+            unpack<T>(now[j], f);
+            if constexpr (KEEP) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    f[j][i] *= rstd;
-                    if (weight) f[j][i] *= g[i];
-                    if (bias) f[j][i] += b[i];
-                }
-                store_clip(yr, c, cols, pack<T>(f[j]));
-            }
+                for (int i = 0; i < V; ++i) { g[i] = kg[j][i]; b[i] = kb[j][i]; }
+            } else params(j, g, b);
+#pragma unroll
+            for (int i = 0; i < V; ++i) f[i] = __builtin_fmaf((f[i] - mean) * rstd, g[i], b[i]);
+            store_raw<T, NT>(yr + column(j), pack<T>(f));
         }
-        if (TPR > 64) __syncthreads();           // the next row's sums go to the same slots
+        if (has_last) yr[last] = (T)__builtin_fmaf((now_last - mean) * rstd, last_g, last_b);
+        // the next row's first sum goes to slots that all have read before this row's second one was whole, and so on
     }
 }
 
@@ -143,6 +180,220 @@ __global__ __launch_bounds__(256) void k_norm_back_rows(NormBackArgs a)
     }
 }
 
+// The same with the gradients of weight and bias in the same pass: TPR threads hold a row (NC vectors each) and add dy * xh and dy of
+// their columns up over all the rows they meet, so that either input is read once.  BT / TPR groups of a block take rows in turn; at the
+// end their sums meet in the LDS in the order of the groups, and the blocks' sums in k_column_sums in the order of the blocks (one block
+// alone: here).  Which rows a group takes depends on the sizes alone.
+// Bound by memory: the next row's vectors are under way while a row is summed.
+// grid (blocks, workers)
+struct NormBackSums {
+    OutTab dweight, dbias;
+    float* partial;              // [worker][block][2][cols]; nullptr: one block a worker
+    int accumulate;
+};
+template <class T, int TPR, int NC, int BT, int NT>
+__global__ __launch_bounds__(BT) void k_norm_back(NormBackArgs a, NormBackSums o)
+{
+    constexpr int V = Vec<T>::N, GROUPS = BT / TPR, IN_WAVE = TPR < 64 ? 64 / TPR : 1, ROUNDS = GROUPS / IN_WAVE;
+    constexpr int WIDTH = TPR * NC * V;
+    __shared__ float slots[2][2][BT / 64];
+    __shared__ float meet[ROUNDS > 1 ? 2 : 1][ROUNDS > 1 ? WIDTH + TPR : 1];      // the last TPR: the elements behind the vectors
+    const uint32_t q = blockIdx.y, rows = a.rows.n[q], cols = a.cols;
+    const uint32_t lane = threadIdx.x % TPR, group = threadIdx.x / TPR, step = gridDim.x * GROUPS;
+    const T* dy = static_cast<const T*>(a.dy.p[q]);
+    const T* x = static_cast<const T*>(a.x.p[q]);
+    T* dx = static_cast<T*>(a.dx.p[q]);
+    const float* weight = static_cast<const float*>(a.weight.p[q]);
+    const float* means = static_cast<const float*>(a.mean.p[q]);
+    const float* rstds = static_cast<const float*>(a.rstd.p[q]);
+    const float count = (float)cols;
+    // whole vectors, and behind the last of them one element a lane
+    const uint32_t main = cols / V * V, last = main + lane;
+    const bool has_last = last < cols;
+    auto column = [&](int j) { return ((uint32_t)j * TPR + lane) * V; };
+    float g[NC][V], sw[NC][V], sb[NC][V];
+    const float last_g = has_last && weight ? weight[last] : 1.0f;
+    float last_sw = 0.0f, last_sb = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) { g[j][i] = 1.0f; sw[j][i] = sb[j][i] = 0.0f; }
+        if (weight && column(j) < main) load_whole<V>(weight + column(j), g[j]);
+    }
+    raw4 ny[NC], nx[NC];
+#pragma unroll
+    for (int j = 0; j < NC; ++j) ny[j] = nx[j] = raw4{0, 0, 0, 0};     // columns behind the row's end stay zero
+    float nm = 0.0f, nr = 0.0f, last_ny = 0.0f, last_nx = 0.0f;
+    auto load_row = [&](uint32_t r) {
+        if (r >= rows) return;
+        nm = means[r];
+        nr = rstds[r];
+        const T *yr = dy + (size_t)r * a.lddy, *xr = x + (size_t)r * a.ldx;
+#pragma unroll
+        for (int j = 0; j < NC; ++j)
+            if (column(j) < main) {
+                ny[j] = load_raw<T, NT>(yr + column(j));
+                nx[j] = load_raw<T, NT>(xr + column(j));
+            }
+        if (has_last) {
+            last_ny = (float)yr[last];
+            last_nx = (float)xr[last];
+        }
+    };
+    uint32_t r = blockIdx.x * GROUPS + group, turn = 0;
+    load_row(r);
+    // a block's groups go through the same number of turns: the sums of a row of more than one wave wait for the whole block
+    for (uint32_t first = blockIdx.x * GROUPS; first < rows; first += step, r += step, turn ^= 1u) {
+        raw4 py[NC], px[NC];
+        const float mean = nm, rstd = nr, last_py = last_ny, last_px = last_nx;
+#pragma unroll
+        for (int j = 0; j < NC; ++j) { py[j] = ny[j]; px[j] = nx[j]; }
+        load_row(r + step);
+        float s1 = 0.0f, s2 = 0.0f;
+        if (r < rows) {                          // a turn without a row adds nothing
+#pragma unroll
+            for (int j = 0; j < NC; ++j) {
+                if (column(j) >= main) continue;
+                float f[V], xh[V];
+                unpack<T>(py[j], f);
+                unpack<T>(px[j], xh);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    xh[i] = (xh[i] - mean) * rstd;
+                    sw[j][i] = __builtin_fmaf(f[i], xh[i], sw[j][i]);
+                    sb[j][i] += f[i];
+                    const float av = f[i] * g[j][i];
+                    s1 += av;
+                    s2 = __builtin_fmaf(av, xh[i], s2);
+                }
+            }
+            if (has_last) {
+                const float xh = (last_px - mean) * rstd, av = last_py * last_g;
+                last_sw = __builtin_fmaf(last_py, xh, last_sw);
+                last_sb += last_py;
+                s1 += av;
+                s2 = __builtin_fmaf(av, xh, s2);
+            }
+        }
+        if (!dx) continue;
+        if constexpr (TPR <= 64) {
+            s1 = group_sum<TPR>(s1, nullptr) / count;
+            s2 = group_sum<TPR>(s2, nullptr) / count;
+        } else {
+            constexpr int W = TPR / 64;
+            s1 = wave_sum_f(s1);
+            s2 = wave_sum_f(s2);
+            float* slot1 = slots[turn][0];
+            float* slot2 = slots[turn][1];
+            if ((threadIdx.x & 63u) == 0) {
+                slot1[threadIdx.x >> 6] = s1;
+                slot2[threadIdx.x >> 6] = s2;
+            }
+            __syncthreads();                     // two turns' slots: nobody is two turns ahead of a reader
+            s1 = slot1[group * W];
+            s2 = slot2[group * W];
+#pragma unroll
+            for (int w = 1; w < W; ++w) {
+                s1 += slot1[group * W + w];
+                s2 += slot2[group * W + w];
+            }
+            s1 /= count;
+            s2 /= count;
+        }
+        if (r >= rows) continue;
+        T* dxr = dx + (size_t)r * a.lddx;
+#pragma unroll
+        for (int j = 0; j < NC; ++j) {
+            if (column(j) >= main) continue;
+            float f[V], xh[V];
+            unpack<T>(py[j], f);
+            unpack<T>(px[j], xh);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                xh[i] = (xh[i] - mean) * rstd;
+                f[i] = rstd * (__builtin_fmaf(f[i], g[j][i], -s1) - xh[i] * s2);
+            }
+            store_raw<T, NT>(dxr + column(j), pack<T>(f));
+        }
+        if (has_last) dxr[last] = (T)(rstd * (__builtin_fmaf(last_py, last_g, -s1) - (last_px - mean) * rstd * s2));
+    }
+    float* outw = static_cast<float*>(o.dweight.p[q]);
+    float* outb = static_cast<float*>(o.dbias.p[q]);
+    const bool want = o.partial || outw || outb;
+    if (!want) return;
+    // groups of one wave first, by exchanges between lanes
+#pragma unroll
+    for (int m = 32; m >= TPR && TPR < 64; m >>= 1)
+#pragma unroll
+        for (int j = 0; j < NC; ++j)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                sw[j][i] += __shfl_xor(sw[j][i], m);
+                sb[j][i] += __shfl_xor(sb[j][i], m);
+            }
+#pragma unroll
+    for (int m = 32; m >= TPR && TPR < 64; m >>= 1) {
+        last_sw += __shfl_xor(last_sw, m);
+        last_sb += __shfl_xor(last_sb, m);
+    }
+    const uint32_t round = group / IN_WAVE;
+    const bool lead = group % IN_WAVE == 0;
+    if constexpr (ROUNDS > 1) {
+        for (uint32_t g0 = 1; g0 < ROUNDS; ++g0) {
+            __syncthreads();
+            if (round == g0 && lead) {
+#pragma unroll
+                for (int j = 0; j < NC; ++j)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        meet[0][(j * V + i) * TPR + lane] = sw[j][i];
+                        meet[1][(j * V + i) * TPR + lane] = sb[j][i];
+                    }
+                meet[0][WIDTH + lane] = last_sw;
+                meet[1][WIDTH + lane] = last_sb;
+            }
+            __syncthreads();
+            if (round == 0 && lead) {
+#pragma unroll
+                for (int j = 0; j < NC; ++j)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        sw[j][i] += meet[0][(j * V + i) * TPR + lane];
+                        sb[j][i] += meet[1][(j * V + i) * TPR + lane];
+                    }
+                last_sw += meet[0][WIDTH + lane];
+                last_sb += meet[1][WIDTH + lane];
+            }
+        }
+    }
+    if (round != 0 || !lead) return;
+    if (o.partial) {
+        outw = o.partial + ((size_t)q * gridDim.x + blockIdx.x) * 2 * cols;
+        outb = outw + cols;
+    }
+    const bool add = !o.partial && o.accumulate;
+    auto put = [&](float* out, auto& v, float l) {
+        if (!out) return;
+#pragma unroll
+        for (int j = 0; j < NC; ++j) {
+            if (column(j) >= main) continue;
+            if (add) {
+                float old[V];
+                load_whole<V>(out + column(j), old);
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[j][i] += old[i];
+            }
+#pragma unroll
+            for (int i = 0; i < V; i += 4)
+                store_raw<float>(out + column(j) + i, raw4{__float_as_uint(v[j][i]), __float_as_uint(v[j][i + 1]), __float_as_uint(v[j][i + 2]),
+                                                           __float_as_uint(v[j][i + 3])});
+        }
+        if (has_last) out[last] = add ? out[last] + l : l;
+    };
+    put(outw, sw, last_sw);
+    put(outb, sb, last_sb);
+}
+
 // ---------------------------------------------------------------------------------------
 // Sums over rows.  A block owns 64 vectors of consecutive columns and a slab of consecutive rows, its four waves every fourth row of it;
 // the slabs' partial sums meet in k_column_sums.  Which rows a slab holds depends on the sizes alone and every sum has a
@@ -159,60 +410,9 @@ struct ColumnArgs {
     int accumulate;
 };
 
-enum : int { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_GELU_TANH = 3, ACT_SILU = 4, ACTS = 5 };
-
-// Slope and value of the activation in binary32.  exp of a large argument is infinite and its reciprocal zero, so that no case is left out;
-// where such a zero would meet an infinite z the factor z is held finite (comparisons let a NaN through).
-__device__ __forceinline__ float act_slope(float z, int act)
-{
-    const float zz = z < -1000.0f ? -1000.0f : (z > 1000.0f ? 1000.0f : z);
-    switch (act) {
-    case ACT_RELU: return z > 0.0f ? 1.0f : 0.0f;
-    case ACT_GELU: return 0.5f * erfcf(zz * -0.70710678118654752f) + zz * expf(-0.5f * zz * zz) * 0.39894228040143268f;
-    case ACT_GELU_TANH: {
-        // 0.5 (1 + tanh u) = 1 / (1 + exp(-2 u)) =: s, its slope in u 2 s (1 - s)
-        const float u2 = 1.5957691216057308f * (zz + 0.044715f * zz * zz * zz);
-        const float s = 1.0f / (1.0f + expf(-u2)), t = 1.0f / (1.0f + expf(u2));
-        return s + zz * s * t * 1.5957691216057308f * (1.0f + 0.134145f * zz * zz);
-    }
-    case ACT_SILU: {
-        const float s = 1.0f / (1.0f + expf(-zz)), t = 1.0f / (1.0f + expf(zz));
-        return s + zz * s * t;
-    }
-    default: return 1.0f;
-    }
-}
-__device__ __forceinline__ float act_value(float z, int act)
-{
-    const float zz = z < -1000.0f ? -1000.0f : z;
-    switch (act) {
-    case ACT_RELU: return z < 0.0f ? 0.0f : z;
-    case ACT_GELU: return 0.5f * zz * erfcf(zz * -0.70710678118654752f);
-    case ACT_GELU_TANH: return zz / (1.0f + expf(-1.5957691216057308f * (zz + 0.044715f * zz * zz * zz)));
-    case ACT_SILU: return zz / (1.0f + expf(-zz));
-    default: return z;
-    }
-}
-
-// The same for several values: one choice for all of them.
-template <int N> __device__ __forceinline__ void act_values(float (&v)[N], int act)
-{
-    auto all = [&](auto f) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = f(v[i]);
-    };
-    switch (act) {
-    case ACT_RELU: all([](float z) { return act_value(z, ACT_RELU); }); break;
-    case ACT_GELU: all([](float z) { return act_value(z, ACT_GELU); }); break;
-    case ACT_GELU_TANH: all([](float z) { return act_value(z, ACT_GELU_TANH); }); break;
-    case ACT_SILU: all([](float z) { return act_value(z, ACT_SILU); }); break;
-    default: break;
-    }
-}
-
 // NORM: out0 = sum dy * xh, out1 = sum dy.  Otherwise dz = dy * act'(z) and out1 = sum dz, from the values before they are rounded.
-template <class T, bool NORM>
-__global__ __launch_bounds__(256) void k_column_grads(ColumnArgs a, int act)
+template <class T, bool NORM, int ACT>
+__global__ __launch_bounds__(256) void k_column_grads(ColumnArgs a)
 {
     constexpr int V = Vec<T>::N, ARR = NORM ? 2 : 1;
     __shared__ float part[3][ARR][V][64];
@@ -241,10 +441,10 @@ __global__ __launch_bounds__(256) void k_column_grads(ColumnArgs a, int act)
                     s1[i] += f[i];
                 }
             } else {
-                if (act != ACT_NONE) {
+                if constexpr (ACT != ACT_NONE) {
                     unpack<T>(load_clip(pb + (size_t)r * a.ldb, c, cols), g);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) f[i] *= act_slope(g[i], act);
+                    for (int i = 0; i < V; ++i) f[i] *= act_slope<ACT>(g[i]);
                 }
                 if (dz) store_clip(dz + (size_t)r * a.lddz, c, cols, pack<T>(f));
 #pragma unroll
@@ -286,7 +486,7 @@ struct ColumnSumArgs {
     const float* partial;
     OutTab out0, out1;
     RowTab rows;
-    uint32_t cols, slab, slabs, arrays;
+    uint32_t cols, slab, slabs, arrays;   // slab 0: every worker has all the slabs
     int accumulate;
 };
 __global__ __launch_bounds__(256) void k_column_sums(ColumnSumArgs a)
@@ -294,7 +494,7 @@ __global__ __launch_bounds__(256) void k_column_sums(ColumnSumArgs a)
     __shared__ float part[16][17];
     const uint32_t q = blockIdx.z, arr = blockIdx.y, tx = threadIdx.x & 15u, ty = threadIdx.x >> 4;
     const uint32_t c = blockIdx.x * 16 + tx;
-    const uint32_t n = max(1u, (a.rows.n[q] + a.slab - 1) / a.slab);
+    const uint32_t n = a.slab ? max(1u, (a.rows.n[q] + a.slab - 1) / a.slab) : a.slabs;
     float s = 0.0f;
     if (c < a.cols)
         for (uint32_t p = ty; p < n; p += 16) s += a.partial[(((size_t)q * a.slabs + p) * a.arrays + arr) * a.cols + c];

@@ -3,6 +3,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <type_traits>
 
 #include "slimdp.h"
 
@@ -64,14 +65,32 @@ template <class T> __device__ __forceinline__ raw4 pack(const float f[Vec<T>::N]
     return p.r;
 }
 
-// Elements [c, c + N) of a row of `cols`: what lies behind the row's end is not touched and reads as zero.
+// Sixteen bytes moved down by k elements (0 < k < Vec<T>::N), zeros behind.
+template <class T> __device__ __forceinline__ raw4 move_down(raw4 v, uint32_t k)
+{
+    const uint32_t words = sizeof(T) == 2 ? k >> 1 : k;
+    if (words & 1u) v = raw4{v.y, v.z, v.w, 0};
+    if (words & 2u) v = raw4{v.z, v.w, 0, 0};
+    if (sizeof(T) == 2) {
+        const uint32_t s = (k & 1u) * 16u;
+        v = raw4{__builtin_amdgcn_alignbit(v.y, v.x, s), __builtin_amdgcn_alignbit(v.z, v.y, s), __builtin_amdgcn_alignbit(v.w, v.z, s), v.w >> s};
+    }
+    return v;
+}
+
+// Elements [c, c + N) of a row of `cols` (c < cols): what lies behind the row's end is not touched and reads as zero.  The last, broken vector
+// of a row is taken from the sixteen bytes that end with the row, and moved down.  (Kernels that hold whole rows in registers take the
+// elements behind the last whole vector one a lane instead: the code for broken vectors costs registers in every vector's place.)
 template <class T, int NT = 0> __device__ __forceinline__ raw4 load_clip(const T* row, uint32_t c, uint32_t cols)
 {
     constexpr uint32_t N = Vec<T>::N;
     if (c + N <= cols) return load_raw<T, NT>(row + c);
+    if (cols >= N) return move_down<T>(load_raw<T, NT>(row + cols - N), c + N - cols);
     Pack<T> p;
+    p.r = raw4{0, 0, 0, 0};
 #pragma unroll
-    for (uint32_t i = 0; i < N; ++i) p.e[i] = c + i < cols ? row[c + i] : (T)0.0f;
+    for (uint32_t i = 0; i < N - 1; ++i)
+        if (i < cols) p.e[i] = row[i];
     return p.r;
 }
 template <class T, int NT = 0> __device__ __forceinline__ void store_clip(T* row, uint32_t c, uint32_t cols, raw4 v)
@@ -85,19 +104,24 @@ template <class T, int NT = 0> __device__ __forceinline__ void store_clip(T* row
         if (c + i < cols) row[c + i] = p.e[i];
 }
 
-// N = Vec<T>::N consecutive binary32 parameters from any address a float may have.
-template <int N> __device__ __forceinline__ void load_params(const float* row, uint32_t c, uint32_t cols, float f[N])
+// N consecutive binary32 parameters from any address a float may have (c < cols).
+template <int N> __device__ __forceinline__ void load_params(const float* row, uint32_t c, uint32_t cols, float (&f)[N])
 {
-    if (c + N <= cols) {
 #pragma unroll
-        for (int i = 0; i < N; i += 4) {
-            const raw4 v = load_raw<float>(row + c + i);
+    for (int i = 0; i < N; i += 4) {
+        const raw4 v = c + i < cols ? load_clip<float>(row, c + i, cols) : raw4{0, 0, 0, 0};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) f[i + j] = __uint_as_float(v[j]);
-        }
-    } else {
+        for (int j = 0; j < 4; ++j) f[i + j] = __uint_as_float(v[j]);
+    }
+}
+
+template <int N> __device__ __forceinline__ void load_whole(const float* p, float (&f)[N])
+{
 #pragma unroll
-        for (int i = 0; i < N; ++i) f[i] = c + i < cols ? row[c + i] : 0.0f;
+    for (int i = 0; i < N; i += 4) {
+        const raw4 v = load_raw<float>(p + i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f[i + j] = __uint_as_float(v[j]);
     }
 }
 

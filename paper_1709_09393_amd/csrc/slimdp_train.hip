@@ -19,6 +19,8 @@ using namespace slimdp;
 namespace {
 
 constexpr uint64_t LD_MAX = 1ull << 32;
+// Streams of more than the last level's 256 MB pass the caches by.
+constexpr uint64_t STREAM_BYTES = 256ull << 20;
 
 // The context's device for the length of a call, whichever is current.
 struct OnDevice {
@@ -127,6 +129,13 @@ struct Call {
                            (unsigned long long)(ws ? have : 0));
         else if (reinterpret_cast<uintptr_t>(ws) % 16) rc = host_fail(ctx, SLIMDP_ERR_INVALID_ARG, "%s: workspace is not aligned to 16 bytes", who);
     }
+    // Bytes of some matrices of this many columns.
+    uint64_t bytes(uint64_t cols, uint64_t matrices) const
+    {
+        uint64_t b = 0;
+        for (uint32_t q = 0; q < W; ++q) b += rows[q] * cols * esize * matrices;
+        return b;
+    }
     template <class P> InTab in(P const* t) const
     {
         InTab r;
@@ -182,6 +191,20 @@ uint64_t column_ws(uint64_t most, uint32_t W, uint64_t cols, size_t es, int arra
     return slabs <= 1 ? 0 : W * slabs * arrays * cols * 4;
 }
 
+// Layer norm's backward pass in one: threads a row, and blocks a worker (256 blocks of 1024 threads, or four times as many of 256, fill
+// the chip; four rows a group at least, so that the sums that the blocks write are few beside the rows).  tpr 0: rows too long to
+// be held beside their sums, two passes.
+struct NormBackShape { uint32_t tpr, block; uint64_t blocks; };
+NormBackShape norm_back_shape(uint64_t most, uint32_t W, uint64_t cols, size_t es)
+{
+    const uint64_t n = ceil_div(cols, 16 / es);
+    const uint32_t tpr = n <= 8 ? 8 : n <= 16 ? 16 : n <= 32 ? 32 : n <= 128 ? 64 : n <= 512 ? 256 : n <= 1024 ? 512 : n <= 2048 ? 1024 : 0;
+    if (!tpr) return {0, 0, 0};
+    const uint32_t block = tpr <= 64 ? 256 : 1024, groups = block / tpr;
+    const uint64_t fill = std::max<uint64_t>(1, (block == 256 ? 1024 : 256) / W);
+    return {tpr, block, std::max<uint64_t>(1, std::min(fill, ceil_div(most, 4 * groups)))};
+}
+
 template <bool NORM> int column_grads(Call& c, ColumnArgs a, uint32_t dtype, int act, void* ws)
 {
     constexpr int ARR = NORM ? 2 : 1;
@@ -191,10 +214,17 @@ template <bool NORM> int column_grads(Call& c, ColumnArgs a, uint32_t dtype, int
     a.partial = a.slabs > 1 ? static_cast<float*>(ws) : nullptr;
     with_type(dtype, [&](auto z) {
         typedef decltype(z) T;
-        c.launched("k_column_grads", [&] {
-            hipLaunchKernelGGL((k_column_grads<T, NORM>), dim3((uint32_t)ceil_div(a.cols, 64 * Vec<T>::N), a.slabs, c.W), dim3(256), 0,
-                               c.v.stream, a, act);
-        });
+        auto launch = [&](auto kernel) {
+            c.launched("k_column_grads", [&] {
+                hipLaunchKernelGGL(kernel, dim3((uint32_t)ceil_div(a.cols, 64 * Vec<T>::N), a.slabs, c.W), dim3(256), 0, c.v.stream, a);
+            });
+        };
+        if constexpr (NORM) launch(k_column_grads<T, true, ACT_NONE>);
+        else if (act == ACT_RELU) launch(k_column_grads<T, false, ACT_RELU>);
+        else if (act == ACT_GELU) launch(k_column_grads<T, false, ACT_GELU>);
+        else if (act == ACT_GELU_TANH) launch(k_column_grads<T, false, ACT_GELU_TANH>);
+        else if (act == ACT_SILU) launch(k_column_grads<T, false, ACT_SILU>);
+        else launch(k_column_grads<T, false, ACT_NONE>);
     });
     if (c.ok() && a.slabs > 1 && (a.out0.p[0] || a.out1.p[0] || NORM)) {
         const ColumnSumArgs s{a.partial, a.out0, a.out1, c.tab, a.cols, a.slab, a.slabs, (uint32_t)ARR, a.accumulate};
@@ -297,28 +327,35 @@ int slimdp_layer_norm(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* rows,
     c.distinct("rstd", rstd, true);
     if (c.ok() && !(eps > 0.0f && std::isfinite(eps))) c.rc = host_fail(ctx, SLIMDP_ERR_INVALID_ARG, "slimdp_layer_norm: eps must be positive and finite");
     if (!c.ok() || c.most == 0) return c.rc;
+    const bool nt = c.bytes(cols, 2) > STREAM_BYTES;
     const NormArgs a{c.in(x), c.in(weight), c.in(bias), c.out(y), c.out(mean), c.out(rstd), c.tab, ldx, ldy, (uint32_t)cols, eps};
     with_type(dtype, [&](auto z) {
         typedef decltype(z) T;
         const uint64_t n = ceil_div(cols, Vec<T>::N);
-        auto launch = [&](auto kernel, uint32_t tpr) {
+        // eight blocks of 256 threads a compute unit (of 256), a block's next row under way while it sums the present one
+        auto launch = [&](auto kernel, auto kernel_nt, uint32_t tpr) {
             const uint32_t block = std::max(tpr, 256u), groups = block / tpr;
-            const uint64_t want = ceil_div(c.most, groups), cap = std::max<uint64_t>(1, 65536 / groups);
+            const uint64_t want = ceil_div(c.most, groups), cap = std::max<uint64_t>(1, 2048 * 256 / block / c.W);
             c.launched("k_norm", [&] {
-                hipLaunchKernelGGL(kernel, dim3((uint32_t)std::min(want, cap), c.W), dim3(block), 0, c.v.stream, a);
+                const dim3 grid((uint32_t)std::min(want, cap), c.W);
+                if (nt) hipLaunchKernelGGL(kernel_nt, grid, dim3(block), 0, c.v.stream, a);
+                else hipLaunchKernelGGL(kernel, grid, dim3(block), 0, c.v.stream, a);
             });
         };
-        if (n <= 8) launch(k_norm<T, 8, 1>, 8);
-        else if (n <= 16) launch(k_norm<T, 16, 1>, 16);
-        else if (n <= 32) launch(k_norm<T, 32, 1>, 32);
-        else if (n <= 64) launch(k_norm<T, 64, 1>, 64);
-        else if (n <= 128) launch(k_norm<T, 64, 2>, 64);
-        else if (n <= 256) launch(k_norm<T, 256, 1>, 256);
-        else if (n <= 512) launch(k_norm<T, 256, 2>, 256);
-        else if (n <= 1024) launch(k_norm<T, 256, 4>, 256);
-        else if (n <= 4096) launch(k_norm<T, 1024, 4>, 1024);
-        else if (n <= 8192) launch(k_norm<T, 1024, 8>, 1024);
-        else if constexpr (Vec<T>::N == 4) launch(k_norm<T, 1024, 16>, 1024);
+#define SLIMDP_NORM(TPR, NC) launch(k_norm<T, TPR, NC, 0>, k_norm<T, TPR, NC, 1>, TPR)
+        if (n <= 8) SLIMDP_NORM(8, 1);
+        else if (n <= 16) SLIMDP_NORM(16, 1);
+        else if (n <= 32) SLIMDP_NORM(32, 1);
+        else if (n <= 64) SLIMDP_NORM(64, 1);
+        else if (n <= 128) SLIMDP_NORM(64, 2);
+        else if (n <= 256) SLIMDP_NORM(256, 1);
+        else if (n <= 512) SLIMDP_NORM(256, 2);
+        else if (n <= 1024) SLIMDP_NORM(256, 4);
+        else if (n <= 2048) SLIMDP_NORM(1024, 2);
+        else if (n <= 4096) SLIMDP_NORM(1024, 4);
+        else if (n <= 8192) SLIMDP_NORM(1024, 8);
+        else if constexpr (Vec<T>::N == 4) SLIMDP_NORM(1024, 16);
+#undef SLIMDP_NORM
     });
     return c.rc;
 }
@@ -326,7 +363,11 @@ int slimdp_layer_norm(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* rows,
 uint64_t slimdp_layer_norm_workspace_bytes(uint32_t n_workers, const uint64_t* rows, uint64_t cols, uint32_t dtype)
 {
     if (!shape_ok(n_workers, rows) || cols == 0 || cols > SLIMDP_MAX_NORM_COLS || dtype > SLIMDP_BF16) return 0;
-    return column_ws(most_rows(n_workers, rows), n_workers, cols, dtype == SLIMDP_F32 ? 4 : 2, 2);
+    const size_t es = dtype == SLIMDP_F32 ? 4 : 2;
+    const uint64_t most = most_rows(n_workers, rows);
+    const NormBackShape s = norm_back_shape(most, n_workers, cols, es);
+    if (s.tpr) return s.blocks > 1 ? n_workers * s.blocks * 2 * cols * 4 : 0;
+    return column_ws(most, n_workers, cols, es, 2);
 }
 
 int slimdp_layer_norm_backward(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* rows, uint64_t cols, uint32_t dtype,
@@ -355,16 +396,52 @@ int slimdp_layer_norm_backward(slimdp_ctx* ctx, uint32_t n_workers, const uint64
     c.distinct("dbias", dbias, false);
     if (sums) c.workspace(workspace, workspace_bytes, slimdp_layer_norm_workspace_bytes(n_workers, rows, cols, dtype));
     if (!c.ok()) return c.rc;
+    const NormBackArgs a{c.in(dy), c.in(x), c.in(weight), c.in(mean), c.in(rstd), c.out(dx), c.tab, lddy, ldx, lddx, (uint32_t)cols};
+    const int accumulate = (flags & SLIMDP_GRAD_ACCUMULATE) != 0;
+    const NormBackShape shape = norm_back_shape(c.most, c.W, cols, c.esize);
+    if (shape.tpr) {
+        if (!sums && c.most == 0) return c.rc;
+        const bool nt = c.bytes(cols, 3) > STREAM_BYTES;
+        const NormBackSums o{c.out(dweight), c.out(dbias), sums && shape.blocks > 1 ? static_cast<float*>(workspace) : nullptr, accumulate};
+        with_type(dtype, [&](auto z) {
+            typedef decltype(z) T;
+            auto launch = [&](auto kernel, auto kernel_nt) {
+                c.launched("k_norm_back", [&] {
+                    const dim3 grid((uint32_t)shape.blocks, c.W);
+                    if (nt) hipLaunchKernelGGL(kernel_nt, grid, dim3(shape.block), 0, c.v.stream, a, o);
+                    else hipLaunchKernelGGL(kernel, grid, dim3(shape.block), 0, c.v.stream, a, o);
+                });
+            };
+            const uint64_t n = ceil_div(cols, Vec<T>::N);
+#define SLIMDP_NORM_BACK(TPR, NC, BT) launch(k_norm_back<T, TPR, NC, BT, 0>, k_norm_back<T, TPR, NC, BT, 1>)
+            if (shape.tpr == 8) SLIMDP_NORM_BACK(8, 1, 256);
+            else if (shape.tpr == 16) SLIMDP_NORM_BACK(16, 1, 256);
+            else if (shape.tpr == 32) SLIMDP_NORM_BACK(32, 1, 256);
+            else if (shape.tpr == 64 && n <= 64) SLIMDP_NORM_BACK(64, 1, 256);
+            else if (shape.tpr == 64) SLIMDP_NORM_BACK(64, 2, 256);
+            else if (shape.tpr == 256 && n <= 256) SLIMDP_NORM_BACK(256, 1, 1024);
+            else if (shape.tpr == 256) SLIMDP_NORM_BACK(256, 2, 1024);
+            else if (shape.tpr == 512) SLIMDP_NORM_BACK(512, 2, 1024);
+            else SLIMDP_NORM_BACK(1024, 2, 1024);
+#undef SLIMDP_NORM_BACK
+        });
+        if (c.ok() && o.partial) {
+            const ColumnSumArgs s{o.partial, o.dweight, o.dbias, c.tab, (uint32_t)cols, 0, (uint32_t)shape.blocks, 2, accumulate};
+            c.launched("k_column_sums", [&] {
+                hipLaunchKernelGGL(k_column_sums, dim3((uint32_t)ceil_div(cols, 16), 2, c.W), dim3(256), 0, c.v.stream, s);
+            });
+        }
+        return c.rc;
+    }
     if (sums) {      // before dx, which may overwrite dy or x
         ColumnArgs s{};
-        s.a = c.in(dy); s.b = c.in(x); s.mean = c.in(mean); s.rstd = c.in(rstd);
+        s.a = a.dy; s.b = a.x; s.mean = a.mean; s.rstd = a.rstd;
         s.out0 = c.out(dweight); s.out1 = c.out(dbias);
         s.lda = lddy; s.ldb = ldx; s.cols = (uint32_t)cols;
-        s.accumulate = (flags & SLIMDP_GRAD_ACCUMULATE) != 0;
+        s.accumulate = accumulate;
         if (column_grads<true>(c, s, dtype, ACT_NONE, workspace)) return c.rc;
     }
     if (!dx || c.most == 0) return c.rc;
-    const NormBackArgs a{c.in(dy), c.in(x), c.in(weight), c.in(mean), c.in(rstd), c.out(dx), c.tab, lddy, ldx, lddx, (uint32_t)cols};
     with_type(dtype, [&](auto z) {
         typedef decltype(z) T;
         c.launched("k_norm_back_rows", [&] {
@@ -522,8 +599,7 @@ int slimdp_distill_loss(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* row
     if (!c.ok() || c.most == 0) return c.rc;
     const DistillArgs a{c.in(logits), c.in(top ? index : nullptr), c.in(top ? value : nullptr), c.in(row_weight), c.out(loss), c.out(lse),
                         c.out(dlogits), c.tab, ldl, ldt, lddl, (uint32_t)vocab, (uint32_t)top, temperature, c.v.status};
-    uint64_t rows_bytes = 0;
-    for (uint32_t q = 0; q < c.W; ++q) rows_bytes += 2 * rows[q] * vocab * c.esize;
+    const uint64_t rows_bytes = c.bytes(vocab, 2);
     with_type(dtype, [&](auto z) {
         typedef decltype(z) T;
         const uint64_t n = ceil_div(vocab, Vec<T>::N);
@@ -535,7 +611,7 @@ int slimdp_distill_loss(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* row
         // the smallest block that holds the row, without a second entry for any thread where the lists are short.  Logits and gradients
         // pass the caches by where they do not fit them: 4 x 1024 rows of 128,000 bf16 (2.1 GB) 533 -> 496 us with stores, 552 without
         // loads that do; but 8 x 4096 rows of 1,000 (131 MB) 62 -> 70.
-        const bool nt = rows_bytes > (256ull << 20);
+        const bool nt = rows_bytes > STREAM_BYTES;
 #define SLIMDP_DISTILL_NT(BT, HELD, MINE)                                                         \
     do { if (nt) launch(k_distill<T, BT, HELD, MINE, 1>, BT); else launch(k_distill<T, BT, HELD, MINE, 0>, BT); } while (0)
 #define SLIMDP_DISTILL(BT, HELD)                                                                  \
