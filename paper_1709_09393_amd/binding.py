@@ -152,9 +152,30 @@ def load() -> C.CDLL:
     return L
 
 
+_arrays = {}
+
+
+def _array(kind, n: int):
+    """The ctypes array type (made once: making it takes longer than filling it)."""
+    got = _arrays.get((kind, n))
+    if got is None:
+        got = _arrays[(kind, n)] = kind * n
+    return got
+
+
 def _u64arr(vals) -> "C.Array":
     vals = [int(v) for v in vals]
-    return (C.c_uint64 * max(1, len(vals)))(*vals)
+    return _array(C.c_uint64, max(1, len(vals)))(*vals)
+
+
+def _dtypes(torch) -> dict:
+    global _dtype_codes
+    if _dtype_codes is None:
+        _dtype_codes = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+    return _dtype_codes
+
+
+_dtype_codes = None
 
 
 def _seg_off(n: int, seg_off) -> "C.Array":
@@ -210,6 +231,8 @@ def select_core_static(score, k: int, core_idx, core_bits, core_off, stream=None
 class SlimDP:
     """One context: n parameters, up to max_workers logical workers, one GPU, one stream."""
 
+    _index = -1          # the device's number as tensors give it
+
     def __init__(self, n: int, max_workers: int, seg_off=None, seed: int = 0, stream=None):
         import torch
         self._torch = torch
@@ -230,6 +253,8 @@ class SlimDP:
             raise SlimDPError(rc, msg)
         self.T = num_tiles(self.n, self.seg_off)
         self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index
+        self._raw_stream = self.stream.cuda_stream
 
     # -- plumbing ------------------------------------------------------------------------
     def _check(self, rc: int) -> None:
@@ -442,14 +467,13 @@ class SlimDP:
     # same for all workers); parameters of the local model and their gradients binary32 and contiguous (pieces of flat vectors).
     def _layout(self, who: str, x: Sequence):
         """(rows of every worker, columns, dtype number, torch dtype) from a call's first list."""
-        torch = self._torch
-        t = x[0]
-        if t.dim() != 2:
+        if x[0].dim() != 2:
             raise ValueError(f"{who}: expected one two-dimensional tensor a worker")
-        code = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}.get(t.dtype)
+        dtype = x[0].dtype
+        code = _dtypes(self._torch).get(dtype)
         if code is None:
-            raise ValueError(f"{who}: unsupported dtype {t.dtype}")
-        return [v.shape[0] for v in x], t.shape[1], code, t.dtype
+            raise ValueError(f"{who}: unsupported dtype {dtype}")
+        return [v.shape[0] for v in x], x[0].shape[1], code, dtype
 
     def _matrix(self, who: str, name: str, ts, rows, cols: int, dtype):
         """Pointer table and row distance of a list of matrices; (None, 0) for none."""
@@ -457,23 +481,23 @@ class SlimDP:
             return None, 0
         if len(ts) != len(rows):
             raise ValueError(f"{who}: {name} holds {len(ts)} tensors for {len(rows)} workers")
-        table, ld = (C.c_void_p * len(ts))(), None
-        for q, t in enumerate(ts):
-            if t.dtype != dtype or t.dim() != 2 or t.shape[0] != rows[q] or t.shape[1] != cols or t.device != self.device:
-                raise ValueError(f"{who}: {name}[{q}] is {tuple(t.shape)} {t.dtype} on {t.device}, "
-                                 f"expected {(rows[q], cols)} {dtype} on {self.device}")
-            if rows[q] == 0:
+        ptrs, ld, device = [], -1, self._index
+        for t, r in zip(ts, rows):                     # a handful of attributes a tensor: small calls wait for this loop
+            if t.dtype is not dtype or t.shape != (r, cols) or t.get_device() != device:
+                raise ValueError(f"{who}: {name}[{len(ptrs)}] is {tuple(t.shape)} {t.dtype} on {t.device}, "
+                                 f"expected {(r, cols)} {dtype} on {self.device}")
+            if r == 0:
+                ptrs.append(None)
                 continue
-            table[q] = t.data_ptr()
             step, inner = t.stride()
             if inner != 1 and cols > 1:
-                raise ValueError(f"{who}: columns of {name}[{q}] are not consecutive")
-            if rows[q] > 1:
-                if ld is None:
-                    ld = step
-                if step != ld or step < cols:
-                    raise ValueError(f"{who}: rows of {name}[{q}] are {step} elements apart, expected {max(ld, cols)}")
-        return table, ld or cols
+                raise ValueError(f"{who}: columns of {name}[{len(ptrs)}] are not consecutive")
+            if r > 1 and step != ld:
+                if ld >= 0 or step < cols:
+                    raise ValueError(f"{who}: rows of {name}[{len(ptrs)}] are {step} elements apart, expected {max(ld, cols)}")
+                ld = step
+            ptrs.append(t.data_ptr())
+        return _array(C.c_void_p, len(ptrs))(*ptrs), max(ld, cols)
 
     def _vectors(self, who: str, name: str, ts, sizes, dtype):
         """Pointer table of a list of contiguous tensors of the given numbers of elements; None for none, also for single workers."""
@@ -481,20 +505,21 @@ class SlimDP:
             return None
         if len(ts) != len(sizes):
             raise ValueError(f"{who}: {name} holds {len(ts)} tensors for {len(sizes)} workers")
-        table = (C.c_void_p * len(ts))()
-        for q, t in enumerate(ts):
-            if t is None:
+        ptrs, device = [], self._index
+        for t, n in zip(ts, sizes):
+            if t is None or (n == 0 and t.numel() == 0):
+                ptrs.append(None)
                 continue
-            if t.dtype != dtype or t.numel() != sizes[q] or t.device != self.device or not t.is_contiguous():
-                raise ValueError(f"{who}: {name}[{q}] is {tuple(t.shape)} {t.dtype} on {t.device}, "
-                                 f"expected {sizes[q]} consecutive {dtype} on {self.device}")
-            table[q] = t.data_ptr() if sizes[q] else None
-        return table
+            if t.dtype is not dtype or t.numel() != n or t.get_device() != device or not t.is_contiguous():
+                raise ValueError(f"{who}: {name}[{len(ptrs)}] is {tuple(t.shape)} {t.dtype} on {t.device}, "
+                                 f"expected {n} consecutive {dtype} on {self.device}")
+            ptrs.append(t.data_ptr())
+        return _array(C.c_void_p, len(ptrs))(*ptrs)
 
     def _new(self, make):
         """Runs make with the context's stream current: memory goes back to the allocator in the order of that stream's work."""
         torch = self._torch
-        if torch.cuda.current_device() == self.device.index and torch.cuda.current_stream().cuda_stream == self.stream.cuda_stream:
+        if torch._C._cuda_getCurrentRawStream(self._index) == self._raw_stream:      # a torch.cuda.Stream object takes ten times as long
             return make()
         with torch.cuda.device(self.device), torch.cuda.stream(self.stream):
             return make()

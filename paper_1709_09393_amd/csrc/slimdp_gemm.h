@@ -34,7 +34,7 @@ __device__ __forceinline__ void copy_to_lds(raw4 r, uint32_t place, uint32_t off
 
 // One operand's tile of a step: X rows (or columns) of the product by 64 of k, as it lies in memory.
 //   k running:      X rows of 128 bytes (whole lines), their eight vectors exchanged by the row's number
-//   KROWS:          64 rows of 2 X bytes, their pieces of 64 bytes exchanged by three bits of the row's number
+//   KROWS:          64 rows of 2 X bytes, their pieces of 64 bytes exchanged by two or three bits of the row's number
 // so that what a wave reads at once lies in different banks.  The copy into the LDS writes a wave's 64 vectors one after the
 // other, so the exchange is made by what each lane asks for.  Vectors outside the matrix are asked for behind the descriptor's end, and
 // arrive as zeros.
@@ -49,7 +49,7 @@ template <bool KROWS, uint32_t X, uint32_t WAVES> struct Tile {
     uint32_t off[LOADS], k[LOADS];
     uint64_t step;
 
-    static __device__ __forceinline__ uint32_t turn(uint32_t k) { return (k & 3u) | ((k >> 1) & 4u); }
+    static __device__ __forceinline__ uint32_t turn(uint32_t k) { return ((k & 3u) | ((k >> 1) & 4u)) & (X / 32 - 1); }
 
     __device__ __forceinline__ void init(const void* p, uint64_t ld, uint32_t x0, uint32_t limit, uint32_t k0)
     {
@@ -174,9 +174,10 @@ __device__ __forceinline__ void epilogue8(const GemmArgs& a, char* c, const T* r
 // two places for either, filled at the end of a step and waited for at the end of the next, the wait took a quarter of the time.)
 // Reads and copies are put between the products one by one: the compiler by itself puts the products first and then waits for the reads.
 // Sums leave through the LDS, WM parts one after the other, so that memory sees whole rows.
+// BLOCKS share a compute unit: one of 256 x 256, or two of 128 x 128.
 // grid (tiles, 1, workers * splits); which tile a block takes goes by the die it runs on (see below).
-template <class T, bool AK, bool BK_, int EPI, uint32_t BM, uint32_t BN, uint32_t WM, uint32_t WN>
-__global__ __launch_bounds__(WM * WN * 64, 1) void k_gemm_tiles(GemmArgs a)
+template <class T, bool AK, bool BK_, int EPI, uint32_t BM, uint32_t BN, uint32_t WM, uint32_t WN, uint32_t BLOCKS>
+__global__ __launch_bounds__(WM * WN * 64, BLOCKS) void k_gemm_tiles(GemmArgs a)
 {
     constexpr uint32_t WAVES = WM * WN, MT = BM / WM, NT = BN / WN, FM = MT / 32, FN = NT / 32;
     typedef Tile<AK, BM, WAVES> TA;

@@ -108,39 +108,39 @@ __device__ __forceinline__ void epilogue4(const GemmArgs& a, uint32_t q, uint32_
     }
 }
 
-// 128 x 128 of C a block of four waves (64 x 64 each, sixteen 16 x 16 accumulators), 128 bytes of k a step.  The next step's
+// S x S of C a block of four waves (a quarter each, in 16 x 16 accumulators), 128 bytes of k a step.  The next step's
 // pieces are loaded into registers while this one's are multiplied from shared memory; there either operand lies with k running,
 // 128 bytes a row, its eight vectors exchanged by the row's number so that the sixteen rows that a read touches meet
 // different banks.  Operands with rows of k are turned over in registers on the way.  Any size, stride and alignment: what lies
-// outside reads as zero.
+// outside reads as zero.  S = 64 where 128 would leave compute units without a block.
 // grid (tiles, 1, workers * splits)
-template <class T, bool AK, bool BK_, int EPI>
+template <class T, bool AK, bool BK_, int EPI, uint32_t S>
 __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
 {
-    constexpr uint32_t V = Vec<T>::N, BM = 128, BN = 128, BK = 8 * V;
-    __shared__ raw4 sa[BM * 8], sb[BN * 8];
+    constexpr uint32_t V = Vec<T>::N, BK = 8 * V, F = S / 32, RUN = S / 32;
+    __shared__ raw4 sa[S * 8], sb[S * 8];
     const uint32_t q = blockIdx.z / a.splits, split = blockIdx.z % a.splits;
     const uint32_t M = a.k_is_rows ? a.M : a.rows.n[q], N = a.N, Kall = a.k_is_rows ? a.rows.n[q] : a.K;
-    const uint32_t across = (N + BN - 1) / BN, m0 = blockIdx.x / across * BM, n0 = blockIdx.x % across * BN;
+    const uint32_t across = (N + S - 1) / S, m0 = blockIdx.x / across * S, n0 = blockIdx.x % across * S;
     if (m0 >= M) return;
     const uint32_t k0 = min(Kall, split * a.k_split), K = min(Kall, k0 + a.k_split);
     const T* A = static_cast<const T*>(a.a.p[q]);
     const T* B = static_cast<const T*>(a.b.p[q]);
     const uint32_t t = threadIdx.x, lane = t & 63u, wave = t >> 6, wm = wave >> 1, wn = wave & 1u;
 
-    // one operand's pieces of a step: four vectors a thread with k running, one square of V x V elements otherwise
-    constexpr uint32_t SQ = BM / V * 8;                            // squares of a tile: 128 or 256
-    constexpr int RA = AK ? (int)V : 4, RB = BK_ ? (int)V : 4;
+    // one operand's pieces of a step: RUN vectors a thread with k running, one square of V x V elements otherwise
+    constexpr uint32_t SQ = S / V * 8;                             // squares of a tile
+    constexpr int RA = AK ? (int)V : (int)RUN, RB = BK_ ? (int)V : (int)RUN;
     raw4 ra[RA], rb[RB];
     auto load = [&](auto krows, const T* P, uint64_t ld, uint32_t x0, uint32_t X, uint32_t kb, uint32_t tt, auto& reg) {
         if constexpr (!decltype(krows)::value) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (uint32_t i = 0; i < RUN; ++i) {
                 const uint32_t x = x0 + (t >> 3) + 32u * i, k = kb + (t & 7u) * V;
                 reg[i] = x < X && k < K ? load_clip(P + (size_t)x * ld, k, K) : raw4{0, 0, 0, 0};
             }
         } else {
-            const uint32_t x = x0 + (tt % (BM / V)) * V, kr = kb + (tt / (BM / V)) * V;
+            const uint32_t x = x0 + (tt % (S / V)) * V, kr = kb + (tt / (S / V)) * V;
 #pragma unroll
             for (uint32_t i = 0; i < V; ++i)
                 reg[i] = tt < SQ && x < X && kr + i < K ? load_clip(P + (size_t)(kr + i) * ld, x, X) : raw4{0, 0, 0, 0};
@@ -149,26 +149,26 @@ __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
     auto put = [&](auto krows, raw4* s, uint32_t tt, auto& reg) {
         if constexpr (!decltype(krows)::value) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (uint32_t i = 0; i < RUN; ++i) {
                 const uint32_t x = (t >> 3) + 32u * i;
                 s[x * 8 + ((t & 7u) ^ (x & 7u))] = reg[i];
             }
         } else if (tt < SQ) {
             transpose<T>(reg);
-            const uint32_t x = (tt % (BM / V)) * V, ck = tt / (BM / V);
+            const uint32_t x = (tt % (S / V)) * V, ck = tt / (S / V);
 #pragma unroll
             for (uint32_t i = 0; i < V; ++i) s[(x + i) * 8 + (ck ^ ((x + i) & 7u))] = reg[i];
         }
     };
     typedef std::integral_constant<bool, AK> ak_t;
     typedef std::integral_constant<bool, BK_> bk_t;
-    // where squares occupy half of the block, the second operand's go to the other half
+    // where squares occupy part of the block, the second operand's go to another part
     const uint32_t ta = t, tb = SQ < 256 && AK ? (t + 128u) & 255u : t;
-    f32x4 acc[4][4];
+    f32x4 acc[F][F];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (uint32_t i = 0; i < F; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (uint32_t j = 0; j < F; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (k0 < K) {
         load(ak_t{}, A, a.lda, m0, M, k0, ta, ra);
         load(bk_t{}, B, a.ldb, n0, N, k0, tb, rb);
@@ -184,28 +184,28 @@ __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
         }
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
-            raw4 fa[4], fb[4];
+            raw4 fa[F], fb[F];
             const uint32_t ch = ks * 4 + (lane >> 4);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t xa = wm * 64 + i * 16 + (lane & 15u), xb = wn * 64 + i * 16 + (lane & 15u);
+            for (uint32_t i = 0; i < F; ++i) {
+                const uint32_t xa = wm * (S / 2) + i * 16 + (lane & 15u), xb = wn * (S / 2) + i * 16 + (lane & 15u);
                 fa[i] = sa[xa * 8 + (ch ^ (xa & 7u))];
                 fb[i] = sb[xb * 8 + (ch ^ (xb & 7u))];
             }
             // B first: a lane then holds four consecutive columns of one row of C
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (uint32_t i = 0; i < F; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = Mma<T>::step(fb[j], fa[i], acc[i][j]);
+                for (uint32_t j = 0; j < F; ++j) acc[i][j] = Mma<T>::step(fb[j], fa[i], acc[i][j]);
         }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t m = m0 + wm * 64 + i * 16 + (lane & 15u);
+    for (uint32_t i = 0; i < F; ++i) {
+        const uint32_t m = m0 + wm * (S / 2) + i * 16 + (lane & 15u);
         if (m >= M) continue;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t n = n0 + wn * 64 + j * 16 + (lane >> 4) * 4;
+        for (uint32_t j = 0; j < F; ++j) {
+            const uint32_t n = n0 + wn * (S / 2) + j * 16 + (lane >> 4) * 4;
             if (n >= N) continue;
             const float s[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
             if (a.splits == 1) epilogue4<T, EPI>(a, q, m, n, N, s);
@@ -217,6 +217,56 @@ __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
             }
         }
     }
+}
+
+// Few rows (up to 16 * MF): the second operand's bytes are all there is to wait for.  It goes from memory to registers as the instructions
+// take it (16 rows, four vectors of each at a time), every element once; a block has 16 of its rows and its eight waves a share of k
+// each, whose sums meet in the LDS in the order of the waves.  A wave asks for eight turns' vectors before it uses the first.
+// grid (ceil(N / 16), 1, workers)
+template <class T, int MF, int EPI>
+__global__ __launch_bounds__(512) void k_gemm_few(GemmArgs a)
+{
+    constexpr uint32_t V = Vec<T>::N, STEP = 4 * V, AHEAD = 8;
+    __shared__ f32x4 meet[8][MF][64];
+    const uint32_t q = blockIdx.z, M = a.rows.n[q], N = a.N, K = a.K, n0 = blockIdx.x * 16;
+    if (M == 0) return;
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, row = lane & 15u, part = (lane >> 4) * V;
+    const T* A = static_cast<const T*>(a.a.p[q]);
+    const T* B = static_cast<const T*>(a.b.p[q]) + (size_t)min(n0 + row, N - 1) * a.ldb;        // rows outside: another's, not kept
+    const uint32_t steps = (K + STEP - 1) / STEP, share = (steps + 7) / 8;
+    const uint32_t s0 = min(steps, wave * share), s1 = min(steps, s0 + share);
+    f32x4 acc[MF];
+#pragma unroll
+    for (int f = 0; f < MF; ++f) acc[f] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (uint32_t s = s0; s < s1; s += AHEAD) {
+        raw4 vb[AHEAD], va[AHEAD][MF];
+#pragma unroll
+        for (uint32_t i = 0; i < AHEAD; ++i) {
+            const uint32_t k = (s + i) * STEP + part;
+            const bool in = s + i < s1 && k < K;
+            vb[i] = in ? load_clip<T, 1>(B, k, K) : raw4{0, 0, 0, 0};
+#pragma unroll
+            for (int f = 0; f < MF; ++f) {
+                const uint32_t m = f * 16 + row;
+                va[i][f] = in && m < M ? load_clip(A + (size_t)m * a.lda, k, K) : raw4{0, 0, 0, 0};
+            }
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < AHEAD; ++i)
+#pragma unroll
+            for (int f = 0; f < MF; ++f) acc[f] = Mma<T>::step(vb[i], va[i][f], acc[f]);
+    }
+#pragma unroll
+    for (int f = 0; f < MF; ++f) meet[wave][f][lane] = acc[f];
+    __syncthreads();
+    if (wave >= MF) return;
+    f32x4 v = meet[0][wave][lane];
+#pragma unroll
+    for (int w = 1; w < 8; ++w) v += meet[w][wave][lane];
+    const uint32_t m = wave * 16 + row, n = n0 + (lane >> 4) * 4;
+    if (m >= M || n >= N) return;
+    const float s[4] = {v[0], v[1], v[2], v[3]};
+    epilogue4<T, EPI>(a, q, m, n, N, s);
 }
 
 // The pieces of split sums, added in order, and the epilogue.  grid (blocks, rows in turn, workers)

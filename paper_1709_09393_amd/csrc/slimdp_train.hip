@@ -238,20 +238,43 @@ template <bool NORM> int column_grads(Call& c, ColumnArgs a, uint32_t dtype, int
 // ---------------------------------------------------------------------------------------
 // products
 // ---------------------------------------------------------------------------------------
+// How a product is cut: the kernel, its tile and the pieces of the sum, by the sizes and the type (and, for the copies into the LDS, the
+// operands' layout; the workspace is asked for as if that did not matter, the larger of both).
 struct Product {
     uint64_t M, N, K;
     uint32_t W;
     size_t es;
-    uint64_t tiles() const { return ceil_div(M, 128) * ceil_div(N, 128); }
-    // Few tiles leave compute units without a block: the sum is then cut, down to four steps a piece.
-    uint64_t splits() const
+    bool rows_of_k;              // K is the number of rows
+
+    struct Cut { uint32_t tile; uint64_t tiles, splits, piece; };
+    uint64_t tiles(uint32_t t) const { return ceil_div(M, t) * ceil_div(N, t); }
+    // The sum in pieces where there are fewer blocks than fill the chip, of four steps at least.
+    Cut cut(uint32_t t, uint64_t slots) const
     {
-        const uint64_t blocks = tiles() * W, steps = ceil_div(K, 128 / es);
-        if (blocks == 0 || blocks >= 256) return 1;
-        return std::max<uint64_t>(1, std::min({512 / blocks, steps / 4, (uint64_t)64}));
+        const uint64_t bk = 128 / es, n = tiles(t), blocks = n * W, steps = ceil_div(K, bk);
+        uint64_t splits = 1;
+        if (blocks && 2 * blocks <= slots) splits = std::max<uint64_t>(1, std::min({slots / blocks, steps / 4, (uint64_t)64}));
+        const uint64_t piece = std::max<uint64_t>(1, ceil_div(steps, splits)) * bk;
+        return {t, n, K ? std::max<uint64_t>(1, ceil_div(K, piece)) : 1, piece};
     }
-    uint64_t piece() const { const uint64_t bk = 128 / es; return std::max<uint64_t>(1, ceil_div(ceil_div(K, bk), splits())) * bk; }
-    uint64_t ws() const { return splits() > 1 ? W * splits() * M * N * 4 : 0; }
+    // Time of a cut in half steps of a 256 x 256 tile: rounds of blocks over the 256 compute units (two at a time of the smaller
+    // tiles), each as many steps as a piece has and what it takes to begin and to write.
+    // (8192^3, and 8 x 2048 x 4096 x 4096 bf16: 256 x 256 1.45 us a step; two of 128 x 128 on a unit 0.95 together.)
+    static double cost(const Cut& c, uint32_t W, uint64_t slots, double step, double ends, size_t es)
+    {
+        return (double)ceil_div(c.tiles * c.splits * W, slots) * ((double)c.piece / (128 / es) * step + ends) + (c.splits > 1 ? 6.0 : 0.0);
+    }
+    // by copies into the LDS: sixteen-bit types
+    Cut copies() const
+    {
+        const Cut big = cut(256, 256), small = cut(128, 512);
+        return cost(big, W, 256, 1.45, 12.0, es) <= cost(small, W, 512, 0.95, 8.0, es) ? big : small;
+    }
+    // through registers: any layout
+    Cut registers() const { return tiles(128) * W >= 384 ? cut(128, 512) : cut(64, 1024); }
+    bool few() const { return !rows_of_k && M <= 64; }
+    static uint64_t bytes(const Cut& c, const Product& p) { return c.splits > 1 ? p.W * c.splits * p.M * p.N * 4 : 0; }
+    uint64_t ws() const { return std::max(bytes(registers(), *this), es == 2 ? bytes(copies(), *this) : 0); }
 };
 
 // Whether the tiles can be copied into the LDS as they lie: whole vectors of sixteen bytes on their own alignment, and
@@ -264,33 +287,53 @@ template <bool AK, bool BK> bool by_copies(const Call& c, const GemmArgs& a, con
             if (reinterpret_cast<uintptr_t>(t.p[q]) % 16) return false;
         return true;
     };
-    return fits(a.a, a.lda, AK ? p.M : p.K) && fits(a.b, a.ldb, BK ? p.N : p.K) && p.splits() == 1 && p.M > 128 && p.N > 128;
+    return p.es == 2 && fits(a.a, a.lda, AK ? p.M : p.K) && fits(a.b, a.ldb, BK ? p.N : p.K);
 }
 
 template <bool AK, bool BK, int EPI> int product(Call& c, GemmArgs a, const Product& p, uint32_t dtype, void* ws)
 {
     if (p.M == 0 || p.N == 0) return c.rc;
-    if (p.tiles() > (1u << 23)) return c.rc = host_fail(c.ctx, SLIMDP_ERR_OUT_OF_RANGE, "%s: more than 2^23 tiles of 128 x 128", c.who);
+    if (p.tiles(64) > (1u << 23)) return c.rc = host_fail(c.ctx, SLIMDP_ERR_OUT_OF_RANGE, "%s: more than 2^23 tiles of 64 x 64", c.who);
     a.rows = c.tab;
     a.M = (uint32_t)p.M; a.N = (uint32_t)p.N; a.K = (uint32_t)p.K;
-    a.splits = (uint32_t)p.splits();
-    a.k_split = (uint32_t)p.piece();
     a.partial = static_cast<float*>(ws);
-    if (dtype != SLIMDP_F32 && by_copies<AK, BK>(c, a, p)) {
-        auto launch = [&](auto z) {
-            typedef decltype(z) T;
-            c.launched("k_gemm_tiles", [&] {
-                hipLaunchKernelGGL((k_gemm_tiles<T, AK, BK, EPI, 256, 256, 2, 2>), dim3((uint32_t)(ceil_div(p.M, 256) * ceil_div(p.N, 256)), 1, c.W * a.splits), dim3(256), 0, c.v.stream, a);
+    a.splits = 1;
+    if constexpr (!AK && !BK) {
+        // few rows against many: 16 rows of weights a block
+        if (p.few() && ceil_div(p.N, 16) * c.W >= 64) {
+            with_type(dtype, [&](auto z) {
+                typedef decltype(z) T;
+                auto launch = [&](auto kernel) {
+                    c.launched("k_gemm_few", [&] {
+                        hipLaunchKernelGGL(kernel, dim3((uint32_t)ceil_div(p.N, 16), 1, c.W), dim3(512), 0, c.v.stream, a);
+                    });
+                };
+                if (p.M <= 16) launch(k_gemm_few<T, 1, EPI>);
+                else if (p.M <= 32) launch(k_gemm_few<T, 2, EPI>);
+                else launch(k_gemm_few<T, 4, EPI>);
             });
-        };
-        if (dtype == SLIMDP_F16) launch(_Float16{}); else launch(__bf16{});
-        return c.rc;
+            return c.rc;
+        }
     }
+    const bool copies = by_copies<AK, BK>(c, a, p);
+    const Product::Cut cut = copies ? p.copies() : p.registers();
+    a.splits = (uint32_t)cut.splits;
+    a.k_split = (uint32_t)cut.piece;
+    const dim3 grid((uint32_t)cut.tiles, 1, c.W * a.splits);
     with_type(dtype, [&](auto z) {
         typedef decltype(z) T;
-        c.launched("k_gemm", [&] {
-            hipLaunchKernelGGL((k_gemm<T, AK, BK, EPI>), dim3((uint32_t)p.tiles(), 1, c.W * a.splits), dim3(256), 0, c.v.stream, a);
-        });
+        if constexpr (sizeof(T) == 2) {
+            if (copies)
+                c.launched("k_gemm_tiles", [&] {
+                    if (cut.tile == 256) hipLaunchKernelGGL((k_gemm_tiles<T, AK, BK, EPI, 256, 256, 2, 2, 1>), grid, dim3(256), 0, c.v.stream, a);
+                    else hipLaunchKernelGGL((k_gemm_tiles<T, AK, BK, EPI, 128, 128, 2, 2, 2>), grid, dim3(256), 0, c.v.stream, a);
+                });
+        }
+        if (!copies)
+            c.launched("k_gemm", [&] {
+                if (cut.tile == 128) hipLaunchKernelGGL((k_gemm<T, AK, BK, EPI, 128>), grid, dim3(256), 0, c.v.stream, a);
+                else hipLaunchKernelGGL((k_gemm<T, AK, BK, EPI, 64>), grid, dim3(256), 0, c.v.stream, a);
+            });
         if (c.ok() && a.splits > 1)
             c.launched("k_gemm_join", [&] {
                 hipLaunchKernelGGL((k_gemm_join<T, EPI>), dim3((uint32_t)ceil_div(p.N, 1024), (uint32_t)std::min<uint64_t>(p.M, 1024), c.W),
@@ -300,9 +343,9 @@ template <bool AK, bool BK, int EPI> int product(Call& c, GemmArgs a, const Prod
     return c.rc;
 }
 
-Product forward_product(uint32_t W, uint64_t most, uint64_t in, uint64_t out, size_t es) { return {most, out, in, W, es}; }
-Product input_product(uint32_t W, uint64_t most, uint64_t in, uint64_t out, size_t es) { return {most, in, out, W, es}; }
-Product weight_product(uint32_t W, uint64_t most, uint64_t in, uint64_t out, size_t es) { return {out, in, most, W, es}; }
+Product forward_product(uint32_t W, uint64_t most, uint64_t in, uint64_t out, size_t es) { return {most, out, in, W, es, false}; }
+Product input_product(uint32_t W, uint64_t most, uint64_t in, uint64_t out, size_t es) { return {most, in, out, W, es, false}; }
+Product weight_product(uint32_t W, uint64_t most, uint64_t in, uint64_t out, size_t es) { return {out, in, most, W, es, true}; }
 
 }  // namespace
 
