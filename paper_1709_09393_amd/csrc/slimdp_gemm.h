@@ -38,7 +38,11 @@ __device__ __forceinline__ void copy_to_lds(raw4 r, uint32_t place, uint32_t off
 // so that what a wave reads at once lies in different banks.  The copy into the LDS writes a wave's 64 vectors one after the
 // other, so the exchange is made by what each lane asks for.  Vectors outside the matrix are asked for behind the descriptor's end, and
 // arrive as zeros.
-template <bool KROWS, uint32_t X, uint32_t WAVES> struct Tile {
+//
+// DIRECT: by copies from memory to the LDS, for operands whose vectors lie on their own alignment.  Otherwise through registers, a
+// step ahead of the LDS, from any address: loads past an edge are made from the last row or vector inside, and what they bring to rows and
+// columns that are not kept does no harm; a last step that k does not fill is written by itself, with zeros (tail).
+template <bool KROWS, uint32_t X, uint32_t WAVES, bool DIRECT, class T> struct Tile {
     static constexpr uint32_t BYTES = X * 2 * GEMM_BK, LOADS = BYTES / 1024 / WAVES;
     static constexpr uint32_t OUT = 0x80000000u;
     static constexpr uint32_t PER_ROW = X / 8, ROWS_A_LOAD = 64 / PER_ROW;           // KROWS: vectors of a row, rows of a load
@@ -48,33 +52,91 @@ template <bool KROWS, uint32_t X, uint32_t WAVES> struct Tile {
     const char* base;            // first row (k running) or first column (KROWS) of the tile
     uint32_t off[LOADS], k[LOADS];
     uint64_t step;
+    // through registers
+    raw4 reg[DIRECT ? 1 : LOADS];
+    uint32_t down[DIRECT || !KROWS ? 1 : LOADS];     // elements by which a vector taken from the row's end is to be moved
+    bool edge;                                       // ... of any lane of the block
+    const T* p;
+    uint64_t ld;
+    uint32_t x0, limit;
 
     static __device__ __forceinline__ uint32_t turn(uint32_t k) { return ((k & 3u) | ((k >> 1) & 4u)) & (X / 32 - 1); }
-
-    __device__ __forceinline__ void init(const void* p, uint64_t ld, uint32_t x0, uint32_t limit, uint32_t k0)
+    // Vector i of a lane: row of the tile in the LDS, and where it begins in it, in elements.
+    static __device__ __forceinline__ void place_of(uint32_t i, uint32_t& r, uint32_t& e)
     {
-        const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-        const uint32_t left = limit - x0;
+        const uint32_t lane = threadIdx.x & 63u, piece = (threadIdx.x >> 6) * LOADS + i;
         if (KROWS) {
-            base = static_cast<const char*>(p) + ((uint64_t)k0 * ld + x0) * 2;
-            step = GEMM_BK * ld * 2;
+            r = piece * ROWS_A_LOAD + lane / PER_ROW;
+            e = ((lane % PER_ROW) ^ (turn(r) << 2)) * 8;
         } else {
-            base = static_cast<const char*>(p) + ((uint64_t)x0 * ld + k0) * 2;
-            step = GEMM_BK * 2;
+            r = piece * 8 + (lane >> 3);
+            e = ((lane & 7u) ^ ((r >> 1) & 7u)) * 8;
+        }
+    }
+
+    // full: whether there is a whole step
+    __device__ __forceinline__ void init(const void* pp, uint64_t ldd, uint32_t x, uint32_t lim, uint32_t k0, bool full)
+    {
+        p = static_cast<const T*>(pp);
+        ld = ldd;
+        x0 = x;
+        limit = lim;
+        const uint32_t left = limit - x0;
+        edge = left < X && limit % 8;
+        base = reinterpret_cast<const char*>(p + (KROWS ? (uint64_t)k0 * ld + x0 : (uint64_t)x0 * ld + k0));
+        step = KROWS ? GEMM_BK * ld * 2 : GEMM_BK * 2;
+        if (!DIRECT && !full) {
+            base = reinterpret_cast<const char*>(p);
+            step = 0;
         }
 #pragma unroll
         for (uint32_t i = 0; i < LOADS; ++i) {
-            const uint32_t piece = wave * LOADS + i;
-            if (KROWS) {
-                const uint32_t r = piece * ROWS_A_LOAD + lane / PER_ROW;
-                const uint32_t x = ((lane % PER_ROW) ^ (turn(r) << 2)) * 8;
-                off[i] = x < left ? (uint32_t)(r * ld * 2) + x * 2 : OUT;
-                k[i] = r;
+            uint32_t r, e;
+            place_of(i, r, e);
+            if (DIRECT) {
+                off[i] = (KROWS ? e : r) < left ? (uint32_t)(r * ld * 2) + e * 2 : OUT;
+                k[i] = KROWS ? r : e;
+            } else if (KROWS) {
+                // the last vector inside where the tile's columns end (it may begin before the tile: then x0 >= 8 - left)
+                const bool inside = e + 8 <= left;
+                down[i] = !inside && e < left ? e + 8 - left : 0u;
+                off[i] = full ? (uint32_t)(r * ld * 2) + (inside ? e : left >= 8 ? left - 8 : 0u) * 2 : 0u;
+                if (!inside && left < 8) down[i] = 0;
             } else {
-                const uint32_t r = piece * 8 + (lane >> 3), c = (lane & 7u) ^ ((r >> 1) & 7u);
-                off[i] = r < left ? (uint32_t)(r * ld * 2) + c * 16 : OUT;
-                k[i] = c * 8;
+                off[i] = full ? (uint32_t)(min(r, left - 1) * ld * 2) + e * 2 : 0u;
             }
+        }
+        if (!DIRECT && KROWS && left < 8) {
+            // fewer columns than a vector are left: take it from before the tile
+            base -= (full ? 8 - left : 0) * 2;
+#pragma unroll
+            for (uint32_t i = 0; i < LOADS; ++i) {
+                uint32_t r, e;
+                place_of(i, r, e);
+                down[i] = e == 0 ? 8 - left : 0u;
+            }
+        }
+    }
+    __device__ __forceinline__ void load(uint32_t i) { reg[i] = load_raw<T>(reinterpret_cast<const T*>(base + off[i])); }
+    // Vector i into its place (place: this wave's part, in bytes from the LDS's start).
+    __device__ __forceinline__ void write(uint32_t i, char* lds, uint32_t place)
+    {
+        raw4 v = reg[i];
+        if constexpr (KROWS)
+            if (edge && down[i]) v = move_down<T>(v, down[i]);
+        *reinterpret_cast<raw4*>(lds + place + i * 1024 + (threadIdx.x & 63u) * 16) = v;
+    }
+    // The step that begins at kb and that k does not fill.
+    __device__ __forceinline__ void tail(char* lds, uint32_t place, uint32_t kb, uint32_t K) const
+    {
+#pragma unroll 1
+        for (uint32_t i = 0; i < LOADS; ++i) {
+            uint32_t r, e;
+            place_of(i, r, e);
+            const uint32_t kk = kb + (KROWS ? r : e), x = x0 + (KROWS ? e : r);
+            raw4 v = {0, 0, 0, 0};
+            if (kk < K && x < limit) v = KROWS ? load_clip(p + (uint64_t)kk * ld, x, limit) : load_clip(p + (uint64_t)x * ld, kk, K);
+            *reinterpret_cast<raw4*>(lds + place + i * 1024 + (threadIdx.x & 63u) * 16) = v;
         }
     }
     // Copy i of the tile at k0 + the steps made so far; kleft: how much of k is left from there.  place: this wave's part.
@@ -176,12 +238,12 @@ __device__ __forceinline__ void epilogue8(const GemmArgs& a, char* c, const T* r
 // Sums leave through the LDS, WM parts one after the other, so that memory sees whole rows.
 // BLOCKS share a compute unit: one of 256 x 256, or two of 128 x 128.
 // grid (tiles, 1, workers * splits); which tile a block takes goes by the die it runs on (see below).
-template <class T, bool AK, bool BK_, int EPI, uint32_t BM, uint32_t BN, uint32_t WM, uint32_t WN, uint32_t BLOCKS>
+template <class T, bool AK, bool BK_, int EPI, uint32_t BM, uint32_t BN, uint32_t WM, uint32_t WN, uint32_t BLOCKS, bool DIRECT>
 __global__ __launch_bounds__(WM * WN * 64, BLOCKS) void k_gemm_tiles(GemmArgs a)
 {
     constexpr uint32_t WAVES = WM * WN, MT = BM / WM, NT = BN / WN, FM = MT / 32, FN = NT / 32;
-    typedef Tile<AK, BM, WAVES> TA;
-    typedef Tile<BK_, BN, WAVES> TB;
+    typedef Tile<AK, BM, WAVES, DIRECT, T> TA;
+    typedef Tile<BK_, BN, WAVES, DIRECT, T> TB;
     constexpr uint32_t PLACES = 3 * TA::BYTES + 2 * TB::BYTES, ROW = BN * 4 + 16, OUT_BYTES = MT * ROW;
     constexpr uint32_t LDS = PLACES > OUT_BYTES ? PLACES : OUT_BYTES;
     __shared__ __attribute__((aligned(1024))) char lds[LDS];
@@ -203,8 +265,9 @@ __global__ __launch_bounds__(WM * WN * 64, BLOCKS) void k_gemm_tiles(GemmArgs a)
 
     TA ta;
     TB tb;
-    ta.init(a.a.p[q], a.lda, m0, M, k0);
-    tb.init(a.b.p[q], a.ldb, n0, N, k0);
+    const uint32_t whole = (K - k0) / GEMM_BK, steps = (K - k0 + GEMM_BK - 1) / GEMM_BK;
+    ta.init(a.a.p[q], a.lda, m0, M, k0, whole != 0);
+    tb.init(a.b.p[q], a.ldb, n0, N, k0, whole != 0);
     f32x16 acc[FM][FN];
 #pragma unroll
     for (uint32_t i = 0; i < FM; ++i)
@@ -214,7 +277,7 @@ __global__ __launch_bounds__(WM * WN * 64, BLOCKS) void k_gemm_tiles(GemmArgs a)
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
     raw4 fa[2][FM], fb[4][FN];
     if (k0 < K) {
-        const uint32_t first = (uint32_t)(uintptr_t)(lds_void*)lds, mine = __builtin_amdgcn_readfirstlane(wave);
+        const uint32_t first = DIRECT ? (uint32_t)(uintptr_t)(lds_void*)lds : 0u, mine = __builtin_amdgcn_readfirstlane(wave);
         const uint32_t first_b = first + 3 * TA::BYTES, my_a = first + mine * TA::PART, my_b = first_b + mine * TB::PART;
         const char* const lds_b = lds + 3 * TA::BYTES;
         // what is left of k where the next copies begin; behind the end zeros are copied, so that every step waits for the same number
@@ -233,8 +296,13 @@ __global__ __launch_bounds__(WM * WN * 64, BLOCKS) void k_gemm_tiles(GemmArgs a)
                 for (uint32_t o = p * EACH; o < (p + 1) * EACH; ++o) {
                     if (o < FM) read_a(a_tile, (KS + 1) & 3u, o);
                     else if (o < R) read_b(b_tile, decltype(bs)::value + (o - FM) / FN, (o - FM) % FN);
-                    else if (o < R + CA) ta.fetch(o - R, a_place, kleft);
-                    else if (o < R + CA + CB) tb.fetch(o - R - CA, b_place, kleft);
+                    else if (o < R + CA) {
+                        if constexpr (DIRECT) ta.fetch(o - R, a_place, kleft);
+                        else { ta.write(o - R, lds, a_place); ta.load(o - R); }
+                    } else if (o < R + CA + CB) {
+                        if constexpr (DIRECT) tb.fetch(o - R - CA, b_place, kleft);
+                        else { tb.write(o - R - CA, lds, b_place); tb.load(o - R - CA); }
+                    }
                 }
                 acc[p / FN][p % FN] = mma32<T>(fb[KS][p % FN], fa[KS & 1][p / FN], acc[p / FN][p % FN]);
                 __builtin_amdgcn_sched_barrier(0);
@@ -246,16 +314,48 @@ __global__ __launch_bounds__(WM * WN * 64, BLOCKS) void k_gemm_tiles(GemmArgs a)
         constexpr std::integral_constant<uint32_t, 3> c3{};
         constexpr std::integral_constant<uint32_t, TA::LOADS> copies_a{};
         constexpr std::integral_constant<uint32_t, TB::LOADS> copies_b{};
+        // through registers: where the next loads come from, the last whole step's place once there is no other
+        uint32_t loaded = 0;
+        auto onward = [&]() {
+            if (++loaded < whole) {
+                ta.next();
+                tb.next();
+            }
+        };
+        auto load_all = [&]() {
+#pragma unroll
+            for (uint32_t i = 0; i < TA::LOADS; ++i) ta.load(i);
+#pragma unroll
+            for (uint32_t i = 0; i < TB::LOADS; ++i) tb.load(i);
+            onward();
+        };
+        auto write_tail = [&](uint32_t step, uint32_t a_place, uint32_t b_place) {
+            if (step == whole && step < steps) {
+                ta.tail(lds, a_place, k0 + step * GEMM_BK, K);
+                tb.tail(lds, b_place, k0 + step * GEMM_BK, K);
+            }
+        };
+        if constexpr (!DIRECT) load_all();
 #pragma unroll
         for (uint32_t st = 0; st < 2; ++st) {
+            if constexpr (DIRECT) {
 #pragma unroll
-            for (uint32_t i = 0; i < TA::LOADS; ++i) ta.fetch(i, my_a + st * TA::BYTES, left(k0 + st * GEMM_BK));
+                for (uint32_t i = 0; i < TA::LOADS; ++i) ta.fetch(i, my_a + st * TA::BYTES, left(k0 + st * GEMM_BK));
 #pragma unroll
-            for (uint32_t i = 0; i < TB::LOADS; ++i) tb.fetch(i, my_b + st * TB::BYTES, left(k0 + st * GEMM_BK));
-            ta.next();
-            tb.next();
+                for (uint32_t i = 0; i < TB::LOADS; ++i) tb.fetch(i, my_b + st * TB::BYTES, left(k0 + st * GEMM_BK));
+                ta.next();
+                tb.next();
+            } else {
+#pragma unroll
+                for (uint32_t i = 0; i < TA::LOADS; ++i) ta.write(i, lds, my_a + st * TA::BYTES);
+#pragma unroll
+                for (uint32_t i = 0; i < TB::LOADS; ++i) tb.write(i, lds, my_b + st * TB::BYTES);
+                load_all();
+                write_tail(st, my_a + st * TA::BYTES, my_b + st * TB::BYTES);
+            }
         }
-        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"(TA::LOADS + TB::LOADS) : "memory");
+        if constexpr (DIRECT) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" :: "n"(TA::LOADS + TB::LOADS) : "memory");
+        else __syncthreads();
 #pragma unroll
         for (uint32_t i = 0; i < FM; ++i) read_a(0, 0, i);
 #pragma unroll
@@ -268,10 +368,16 @@ __global__ __launch_bounds__(WM * WN * 64, BLOCKS) void k_gemm_tiles(GemmArgs a)
             __builtin_amdgcn_sched_barrier(0);
             quarter(c1, a_now, 0, c0, c0, copies_a, c0, my_a + a_after, 0, more);
             quarter(c2, a_now, 0, c0, c0, c0, copies_b, 0, my_b + b_now, more);
-            ta.next();
-            tb.next();
             // the next step's tiles have arrived, and every wave has read all of this one's
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(TA::LOADS + TB::LOADS) : "memory");
+            if constexpr (DIRECT) {
+                ta.next();
+                tb.next();
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(TA::LOADS + TB::LOADS) : "memory");
+            } else {
+                onward();
+                write_tail((kb - k0) / GEMM_BK + 2, my_a + a_after, my_b + b_now);
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            }
             __builtin_amdgcn_sched_barrier(0);
             b_now ^= TB::BYTES;
             quarter(c3, a_next, b_now, c0, c2, c0, c0, 0, 0, 0);
@@ -280,7 +386,7 @@ __global__ __launch_bounds__(WM * WN * 64, BLOCKS) void k_gemm_tiles(GemmArgs a)
             a_next = a_after;
             a_after = t;
         }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");          // no copy may land in what follows
+        if constexpr (DIRECT) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");          // no copy may land in what follows
     }
     char* out = static_cast<char*>(a.c.p[q]);
     const T* res = EPI == 0 ? static_cast<const T*>(a.residual.p[q]) : nullptr;

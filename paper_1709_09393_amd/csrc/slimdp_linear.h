@@ -132,32 +132,57 @@ __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
     constexpr uint32_t SQ = S / V * 8;                             // squares of a tile
     constexpr int RA = AK ? (int)V : (int)RUN, RB = BK_ ? (int)V : (int)RUN;
     raw4 ra[RA], rb[RB];
+    // Every load is made, from a place inside the matrix (the last row or vector in place of what lies outside), and what does not belong is
+    // cleared when it is put into the LDS: a load behind a condition of its own waits for the ones before it (2048 x 4096 x 4096 bf16 with
+    // rows of k for either operand 368 us).  Matrices narrower than a vector are read element by element.
+    const bool narrow = (AK ? M : Kall) < V || (BK_ ? N : Kall) < V;
     auto load = [&](auto krows, const T* P, uint64_t ld, uint32_t x0, uint32_t X, uint32_t kb, uint32_t tt, auto& reg) {
         if constexpr (!decltype(krows)::value) {
 #pragma unroll
             for (uint32_t i = 0; i < RUN; ++i) {
                 const uint32_t x = x0 + (t >> 3) + 32u * i, k = kb + (t & 7u) * V;
-                reg[i] = x < X && k < K ? load_clip(P + (size_t)x * ld, k, K) : raw4{0, 0, 0, 0};
+                if (narrow) reg[i] = x < X && k < K ? load_clip(P + (size_t)x * ld, k, K) : raw4{0, 0, 0, 0};
+                else reg[i] = load_raw<T>(P + (size_t)min(x, X - 1) * ld + min(k, Kall - V));
             }
         } else {
-            const uint32_t x = x0 + (tt % (S / V)) * V, kr = kb + (tt / (S / V)) * V;
+            if (tt >= SQ) return;
+            const uint32_t x = x0 + (tt >> 3) * V, kr = kb + (tt & 7u) * V;        // eight lanes: a whole row of the LDS to write
 #pragma unroll
-            for (uint32_t i = 0; i < V; ++i)
-                reg[i] = tt < SQ && x < X && kr + i < K ? load_clip(P + (size_t)(kr + i) * ld, x, X) : raw4{0, 0, 0, 0};
+            for (uint32_t i = 0; i < V; ++i) {
+                if (narrow) reg[i] = x < X && kr + i < K ? load_clip(P + (size_t)(kr + i) * ld, x, X) : raw4{0, 0, 0, 0};
+                else reg[i] = load_raw<T>(P + (size_t)min(kr + i, K - 1) * ld + min(x, X - V));
+            }
         }
     };
-    auto put = [&](auto krows, raw4* s, uint32_t tt, auto& reg) {
+    auto put = [&](auto krows, raw4* s, uint32_t x0, uint32_t X, uint32_t kb, uint32_t tt, auto& reg) {
         if constexpr (!decltype(krows)::value) {
+            const uint32_t k = kb + (t & 7u) * V;
 #pragma unroll
             for (uint32_t i = 0; i < RUN; ++i) {
                 const uint32_t x = (t >> 3) + 32u * i;
-                s[x * 8 + ((t & 7u) ^ (x & 7u))] = reg[i];
+                if (!narrow) {
+                    if (k < K && k + V > K) reg[i] = move_down<T>(reg[i], k + V - K);
+                    if (k >= K || x0 + x >= X) reg[i] = raw4{0, 0, 0, 0};
+                }
+                s[x * 8 + ((t & 7u) ^ ((x >> 1) & 7u))] = reg[i];
             }
         } else if (tt < SQ) {
-            transpose<T>(reg);
-            const uint32_t x = (tt % (S / V)) * V, ck = tt / (S / V);
+            const uint32_t x = (tt >> 3) * V, ck = tt & 7u, kr = kb + ck * V;
+            if (!narrow) {
+                const uint32_t end = x0 + x + V;
+                if (end > X) {
 #pragma unroll
-            for (uint32_t i = 0; i < V; ++i) s[(x + i) * 8 + (ck ^ ((x + i) & 7u))] = reg[i];
+                    for (uint32_t i = 0; i < V; ++i) reg[i] = end < X + V ? move_down<T>(reg[i], end - X) : raw4{0, 0, 0, 0};
+                }
+                if (kr + V > K) {
+#pragma unroll
+                    for (uint32_t i = 0; i < V; ++i)
+                        if (kr + i >= K) reg[i] = raw4{0, 0, 0, 0};
+                }
+            }
+            transpose<T>(reg);
+#pragma unroll
+            for (uint32_t i = 0; i < V; ++i) s[(x + i) * 8 + (ck ^ (((x + i) >> 1) & 7u))] = reg[i];
         }
     };
     typedef std::integral_constant<bool, AK> ak_t;
@@ -175,8 +200,8 @@ __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
     }
     for (uint32_t kb = k0; kb < K; kb += BK) {
         __syncthreads();
-        put(ak_t{}, sa, ta, ra);
-        put(bk_t{}, sb, tb, rb);
+        put(ak_t{}, sa, m0, M, kb, ta, ra);
+        put(bk_t{}, sb, n0, N, kb, tb, rb);
         __syncthreads();
         if (kb + BK < K) {
             load(ak_t{}, A, a.lda, m0, M, kb + BK, ta, ra);
@@ -189,8 +214,8 @@ __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
 #pragma unroll
             for (uint32_t i = 0; i < F; ++i) {
                 const uint32_t xa = wm * (S / 2) + i * 16 + (lane & 15u), xb = wn * (S / 2) + i * 16 + (lane & 15u);
-                fa[i] = sa[xa * 8 + (ch ^ (xa & 7u))];
-                fb[i] = sb[xb * 8 + (ch ^ (xb & 7u))];
+                fa[i] = sa[xa * 8 + (ch ^ ((xa >> 1) & 7u))];
+                fb[i] = sb[xb * 8 + (ch ^ ((xb >> 1) & 7u))];
             }
             // B first: a lane then holds four consecutive columns of one row of C
 #pragma unroll

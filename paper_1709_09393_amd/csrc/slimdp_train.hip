@@ -246,48 +246,57 @@ struct Product {
     size_t es;
     bool rows_of_k;              // K is the number of rows
 
-    struct Cut { uint32_t tile; uint64_t tiles, splits, piece; };
+    struct Cut { uint32_t tile; uint64_t tiles, splits, piece; double us; };
     uint64_t tiles(uint32_t t) const { return ceil_div(M, t) * ceil_div(N, t); }
-    // The sum in pieces where there are fewer blocks than fill the chip, of four steps at least.
-    Cut cut(uint32_t t, uint64_t slots) const
+    // What a cut takes, as measured: `slots` blocks run at a time over the 256 compute units, `step` us for a step of all of them (less
+    // where there is one block to a unit at most), `ends` us to begin and to write, and where the sum is cut the pieces' way to memory and back at
+    // 4 TB/s.  Products of 8192 x 8192 x 8192 and 8 x 2048 x 4096 x 4096, bf16: 1.45 us a step with 256 x 256, 0.95 with two of 128 x 128;
+    // through registers 1.9, binary32 3.6; a quarter of that and four blocks with 64 x 64.
+    struct Kernel { uint32_t tile, slots; double step, alone, ends; };
+    Cut cut(const Kernel& k, uint64_t want) const
     {
-        const uint64_t bk = 128 / es, n = tiles(t), blocks = n * W, steps = ceil_div(K, bk);
-        uint64_t splits = 1;
-        if (blocks && 2 * blocks <= slots) splits = std::max<uint64_t>(1, std::min({slots / blocks, steps / 4, (uint64_t)64}));
-        const uint64_t piece = std::max<uint64_t>(1, ceil_div(steps, splits)) * bk;
-        return {t, n, K ? std::max<uint64_t>(1, ceil_div(K, piece)) : 1, piece};
+        const uint64_t bk = 128 / es, steps = ceil_div(K, bk), per = std::max<uint64_t>(1, ceil_div(steps, want));
+        const uint64_t splits = std::max<uint64_t>(1, ceil_div(steps, per)), blocks = tiles(k.tile) * W * splits;
+        const double step = blocks <= 256 ? k.alone : k.step;
+        double us = (double)ceil_div(blocks, k.slots) * ((double)per * step + k.ends);
+        if (splits > 1) us += 4.0 + (double)(W * splits * M * N) * 8.0 / 4e6;
+        return {k.tile, tiles(k.tile), splits, per * bk, us};
     }
-    // Time of a cut in half steps of a 256 x 256 tile: rounds of blocks over the 256 compute units (two at a time of the smaller
-    // tiles), each as many steps as a piece has and what it takes to begin and to write.
-    // (8192^3, and 8 x 2048 x 4096 x 4096 bf16: 256 x 256 1.45 us a step; two of 128 x 128 on a unit 0.95 together.)
-    static double cost(const Cut& c, uint32_t W, uint64_t slots, double step, double ends, size_t es)
+    Cut best(const Kernel& big, const Kernel& small) const
     {
-        return (double)ceil_div(c.tiles * c.splits * W, slots) * ((double)c.piece / (128 / es) * step + ends) + (c.splits > 1 ? 6.0 : 0.0);
+        Cut b = cut(big, 1);
+        for (const uint64_t want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64})
+            for (const Kernel* k : {&big, &small}) {
+                const Cut c = cut(*k, want);
+                if (c.us < b.us) b = c;
+            }
+        return b;
     }
     // by copies into the LDS: sixteen-bit types
-    Cut copies() const
-    {
-        const Cut big = cut(256, 256), small = cut(128, 512);
-        return cost(big, W, 256, 1.45, 12.0, es) <= cost(small, W, 512, 0.95, 8.0, es) ? big : small;
-    }
+    Cut copies() const { return best({256, 256, 1.45, 1.45, 12.0}, {128, 512, 0.95, 0.65, 8.0}); }
     // through registers: any layout
-    Cut registers() const { return tiles(128) * W >= 384 ? cut(128, 512) : cut(64, 1024); }
+    Cut registers() const
+    {
+        const double f = es == 4 ? 3.6 : 1.9;
+        return best({128, 512, f, 0.6 * f, 8.0}, {64, 1024, 0.55 * f, 0.2 * f, 6.0});
+    }
     bool few() const { return !rows_of_k && M <= 64; }
     static uint64_t bytes(const Cut& c, const Product& p) { return c.splits > 1 ? p.W * c.splits * p.M * p.N * 4 : 0; }
     uint64_t ws() const { return std::max(bytes(registers(), *this), es == 2 ? bytes(copies(), *this) : 0); }
 };
 
-// Whether the tiles can be copied into the LDS as they lie: whole vectors of sixteen bytes on their own alignment, and
-// distances that fit the copies' offsets.
-template <bool AK, bool BK> bool by_copies(const Call& c, const GemmArgs& a, const Product& p)
+// How the tile kernel takes sixteen-bit operands: not at all (2: rows shorter than a vector, or distances that do not fit its offsets), through
+// registers (1), or copied into the LDS as they lie (0: whole vectors on their own alignment).
+template <bool AK, bool BK> int staging(const Call& c, const GemmArgs& a, const Product& p)
 {
-    auto fits = [&](const InTab& t, uint64_t ld, uint64_t run) {
-        if (ld % 8 || run % 8 || ld > (1u << 21)) return false;
+    auto of = [&](const InTab& t, uint64_t ld, uint64_t run) {
+        if (run < 8 || ld > (1u << 21)) return 2;
+        if (ld % 8 || run % 8) return 1;
         for (uint32_t q = 0; q < c.W; ++q)
-            if (reinterpret_cast<uintptr_t>(t.p[q]) % 16) return false;
-        return true;
+            if (reinterpret_cast<uintptr_t>(t.p[q]) % 16) return 1;
+        return 0;
     };
-    return p.es == 2 && fits(a.a, a.lda, AK ? p.M : p.K) && fits(a.b, a.ldb, BK ? p.N : p.K);
+    return p.es == 2 ? std::max(of(a.a, a.lda, AK ? p.M : p.K), of(a.b, a.ldb, BK ? p.N : p.K)) : 2;
 }
 
 template <bool AK, bool BK, int EPI> int product(Call& c, GemmArgs a, const Product& p, uint32_t dtype, void* ws)
@@ -315,21 +324,23 @@ template <bool AK, bool BK, int EPI> int product(Call& c, GemmArgs a, const Prod
             return c.rc;
         }
     }
-    const bool copies = by_copies<AK, BK>(c, a, p);
-    const Product::Cut cut = copies ? p.copies() : p.registers();
+    const int stage = staging<AK, BK>(c, a, p);
+    const Product::Cut cut = stage < 2 ? p.copies() : p.registers();
     a.splits = (uint32_t)cut.splits;
     a.k_split = (uint32_t)cut.piece;
     const dim3 grid((uint32_t)cut.tiles, 1, c.W * a.splits);
     with_type(dtype, [&](auto z) {
         typedef decltype(z) T;
         if constexpr (sizeof(T) == 2) {
-            if (copies)
-                c.launched("k_gemm_tiles", [&] {
-                    if (cut.tile == 256) hipLaunchKernelGGL((k_gemm_tiles<T, AK, BK, EPI, 256, 256, 2, 2, 1>), grid, dim3(256), 0, c.v.stream, a);
-                    else hipLaunchKernelGGL((k_gemm_tiles<T, AK, BK, EPI, 128, 128, 2, 2, 2>), grid, dim3(256), 0, c.v.stream, a);
-                });
+            auto launch = [&](auto kernel) {
+                c.launched("k_gemm_tiles", [&] { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, c.v.stream, a); });
+            };
+            if (stage == 0 && cut.tile == 256) launch(k_gemm_tiles<T, AK, BK, EPI, 256, 256, 2, 2, 1, true>);
+            else if (stage == 0) launch(k_gemm_tiles<T, AK, BK, EPI, 128, 128, 2, 2, 2, true>);
+            else if (stage == 1 && cut.tile == 256) launch(k_gemm_tiles<T, AK, BK, EPI, 256, 256, 2, 2, 1, false>);
+            else if (stage == 1) launch(k_gemm_tiles<T, AK, BK, EPI, 128, 128, 2, 2, 2, false>);
         }
-        if (!copies)
+        if (stage == 2)
             c.launched("k_gemm", [&] {
                 if (cut.tile == 128) hipLaunchKernelGGL((k_gemm<T, AK, BK, EPI, 128>), grid, dim3(256), 0, c.v.stream, a);
                 else hipLaunchKernelGGL((k_gemm<T, AK, BK, EPI, 64>), grid, dim3(256), 0, c.v.stream, a);

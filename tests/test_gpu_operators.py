@@ -389,18 +389,20 @@ def test_linear_backward_matches_the_formula(ctx, dtype, pad, shift):
         mk.check_gaps()
 
 
-def test_products_larger_than_a_wave_of_tiles(ctx):
-    """Every tile shape and the whole chip busy; spot rows and columns against 64 bits."""
-    mk = Maker(9)
+@pytest.mark.parametrize("R,K,N,pad,shift", [(2100, 1032, 2312, 0, 0), (4104, 1032, 4360, 8, 8), (2101, 1033, 2311, 0, 0), (4097, 1027, 4355, 1, 1),
+                                             (4099, 60, 4102, 0, 0), (64, 4352, 4104, 0, 0), (4100, 4101, 190, 2, 0), (700, 9000, 130, 0, 0)])
+def test_products_larger_than_a_wave_of_tiles(ctx, R, K, N, pad, shift):
+    """Every tile size, both ways into the LDS, the whole chip busy and the sum in pieces; every element against 64 bits."""
     for t in (torch.bfloat16, torch.float16):
-        x, w, dz = mk.normal(2100, 1032, t), mk.normal(2312, 1032, t, 0.03), mk.normal(2100, 2312, t, 0.1)
+        mk = Maker(9, pad, shift)
+        x, w, dz = mk.normal(R, K, t), mk.normal(N, K, t, 0.03), mk.normal(R, N, t, 0.1)
         y, _ = ctx.linear([x], [w])
         dx, dw = ctx.linear_backward([dz], [x], [w])
         ctx.synchronize()
-        for ref, mag, got, K, ut in ((x.double() @ w.double().t(), x.double().abs() @ w.double().abs().t(), y[0], 1032, u(t)),
-                                     (dz.double() @ w.double(), dz.double().abs() @ w.double().abs(), dx[0], 2312, u(t)),
-                                     (dz.double().t() @ x.double(), dz.double().abs().t() @ x.double().abs(), dw[0], 2100, F)):
-            close(got, ref, ut * ref.abs() + 1.01 * steps(K, t) * F * mag + tiny(t), str(t))
+        for ref, mag, got, n, ut in ((x.double() @ w.double().t(), x.double().abs() @ w.double().abs().t(), y[0], K, u(t)),
+                                     (dz.double() @ w.double(), dz.double().abs() @ w.double().abs(), dx[0], N, u(t)),
+                                     (dz.double().t() @ x.double(), dz.double().abs().t() @ x.double().abs(), dw[0], R, F)):
+            close(got, ref, ut * ref.abs() + 1.01 * steps(n, t) * F * mag + tiny(t), str(t))
 
 
 def test_rows_behind_infinite_and_nan_neighbours_stay_clean(ctx):
