@@ -99,13 +99,14 @@ struct Call {
         if (!p && needed) rc = host_fail(ctx, SLIMDP_ERR_INVALID_ARG, "%s: %s[%u] is NULL", who, what, q);
         else if (reinterpret_cast<uintptr_t>(p) % es) rc = host_fail(ctx, SLIMDP_ERR_INVALID_ARG, "%s: %s[%u] is not aligned to its elements", who, what, q);
     }
-    // Outputs that may not be the given input; same: unless rows lie the same distance apart.
-    template <class P, class R> void apart(const char* wa, P const* a, const char* wb, R const* b, bool same = false)
+    // Outputs that may not be the given array; own: but for the same worker's.  per_row: matrices with a row for each of the worker's.
+    template <class P, class R> void apart(const char* wa, P const* a, const char* wb, R const* b, bool own = false, bool per_row = true)
     {
-        if (!ok() || !a || !b || same) return;
+        if (!ok() || !a || !b) return;
         for (uint32_t q = 0; q < W; ++q)
             for (uint32_t o = 0; o < W; ++o)
-                if (a[q] && rows[q] && rows[o] && static_cast<const void*>(a[q]) == static_cast<const void*>(b[o])) {
+                if (a[q] && (!per_row || (rows[q] && rows[o])) && !(own && q == o) &&
+                    static_cast<const void*>(a[q]) == static_cast<const void*>(b[o])) {
                     rc = host_fail(ctx, SLIMDP_ERR_INVALID_ARG, "%s: %s[%u] is %s[%u]", who, wa, q, wb, o);
                     return;
                 }
@@ -205,13 +206,14 @@ NormBackShape norm_back_shape(uint64_t most, uint32_t W, uint64_t cols, size_t e
     return {tpr, block, std::max<uint64_t>(1, std::min(fill, ceil_div(most, 4 * groups)))};
 }
 
-template <bool NORM> int column_grads(Call& c, ColumnArgs a, uint32_t dtype, int act, void* ws)
+// ws: for the slabs' sums; nullptr where no sums are asked for.
+template <bool NORM> int column_grads(Call& c, ColumnArgs a, uint32_t dtype, int act, bool sums, void* ws)
 {
     constexpr int ARR = NORM ? 2 : 1;
     a.rows = c.tab;
     a.slab = (uint32_t)slab_rows(c.most, c.W, a.cols, c.esize);
     a.slabs = (uint32_t)std::max<uint64_t>(1, ceil_div(c.most, a.slab));
-    a.partial = a.slabs > 1 ? static_cast<float*>(ws) : nullptr;
+    a.partial = sums && a.slabs > 1 ? static_cast<float*>(ws) : nullptr;
     with_type(dtype, [&](auto z) {
         typedef decltype(z) T;
         auto launch = [&](auto kernel) {
@@ -226,7 +228,7 @@ template <bool NORM> int column_grads(Call& c, ColumnArgs a, uint32_t dtype, int
         else if (act == ACT_SILU) launch(k_column_grads<T, false, ACT_SILU>);
         else launch(k_column_grads<T, false, ACT_NONE>);
     });
-    if (c.ok() && a.slabs > 1 && (a.out0.p[0] || a.out1.p[0] || NORM)) {
+    if (c.ok() && a.partial) {
         const ColumnSumArgs s{a.partial, a.out0, a.out1, c.tab, a.cols, a.slab, a.slabs, (uint32_t)ARR, a.accumulate};
         c.launched("k_column_sums", [&] {
             hipLaunchKernelGGL(k_column_sums, dim3((uint32_t)ceil_div(a.cols, 16), ARR, c.W), dim3(256), 0, c.v.stream, s);
@@ -379,6 +381,7 @@ int slimdp_layer_norm(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* rows,
     c.distinct("y", y, true);
     c.distinct("mean", mean, true);
     c.distinct("rstd", rstd, true);
+    c.apart("mean", mean, "rstd", rstd);
     if (c.ok() && !(eps > 0.0f && std::isfinite(eps))) c.rc = host_fail(ctx, SLIMDP_ERR_INVALID_ARG, "slimdp_layer_norm: eps must be positive and finite");
     if (!c.ok() || c.most == 0) return c.rc;
     const bool nt = c.bytes(cols, 2) > STREAM_BYTES;
@@ -448,6 +451,7 @@ int slimdp_layer_norm_backward(slimdp_ctx* ctx, uint32_t n_workers, const uint64
     c.distinct("dx", dx, true);
     c.distinct("dweight", dweight, false);
     c.distinct("dbias", dbias, false);
+    c.apart("dweight", dweight, "dbias", dbias, false, false);
     if (sums) c.workspace(workspace, workspace_bytes, slimdp_layer_norm_workspace_bytes(n_workers, rows, cols, dtype));
     if (!c.ok()) return c.rc;
     const NormBackArgs a{c.in(dy), c.in(x), c.in(weight), c.in(mean), c.in(rstd), c.out(dx), c.tab, lddy, ldx, lddx, (uint32_t)cols};
@@ -493,7 +497,7 @@ int slimdp_layer_norm_backward(slimdp_ctx* ctx, uint32_t n_workers, const uint64
         s.out0 = c.out(dweight); s.out1 = c.out(dbias);
         s.lda = lddy; s.ldb = ldx; s.cols = (uint32_t)cols;
         s.accumulate = accumulate;
-        if (column_grads<true>(c, s, dtype, ACT_NONE, workspace)) return c.rc;
+        if (column_grads<true>(c, s, dtype, ACT_NONE, true, workspace)) return c.rc;
     }
     if (!dx || c.most == 0) return c.rc;
     with_type(dtype, [&](auto z) {
@@ -578,7 +582,7 @@ int slimdp_linear_epilogue_backward(slimdp_ctx* ctx, uint32_t n_workers, const u
     s.a = c.in(dy); s.b = c.in(z); s.dz = c.out(dz); s.out1 = c.out(dbias);
     s.lda = lddy; s.ldb = ldz; s.lddz = lddz; s.cols = (uint32_t)out;
     s.accumulate = (flags & SLIMDP_GRAD_ACCUMULATE) != 0;
-    return column_grads<false>(c, s, dtype, (int)activation, workspace);
+    return column_grads<false>(c, s, dtype, (int)activation, dbias != nullptr, workspace);
 }
 
 int slimdp_linear_backward(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* rows, uint64_t in, uint64_t out, uint32_t dtype,
@@ -648,7 +652,8 @@ int slimdp_distill_loss(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* row
     c.distinct("dlogits", dlogits, true);
     c.distinct("loss", loss, true);
     c.distinct("lse", lse, true);
-    if (c.ok() && !(temperature > 0.0f && std::isfinite(temperature) && std::isfinite(1.0f / temperature)))
+    c.apart("loss", loss, "lse", lse);
+    if (c.ok() && !(temperature > 0.0f && std::isfinite(temperature) && std::isfinite(LOG2E / temperature)))
         c.rc = host_fail(ctx, SLIMDP_ERR_INVALID_ARG, "slimdp_distill_loss: temperature must be positive and finite");
     if (!c.ok() || c.most == 0) return c.rc;
     const DistillArgs a{c.in(logits), c.in(top ? index : nullptr), c.in(top ? value : nullptr), c.in(row_weight), c.out(loss), c.out(lse),

@@ -427,6 +427,27 @@ def test_rows_behind_infinite_and_nan_neighbours_stay_clean(ctx):
     assert not bool(y[0][5].isfinite().any()) and bool(torch.cat([y[0][:5], y[0][6:]]).isfinite().all())
 
 
+def test_epilogue_backward_writes_no_sums_that_are_not_asked_for(ctx):
+    """Without the bias's gradient a workspace is not touched, however small; workers that want none beside ones that do."""
+    import ctypes as C
+    mk = Maker(12)
+    dy, z, out = [mk.normal(4000, 48, torch.float32) for _ in range(2)], [mk.normal(4000, 48, torch.float32) for _ in range(2)], mk.vec(48)
+    want = ctx.linear_epilogue_backward(dy, z, "silu")
+    need = ctx._L.slimdp_linear_workspace_bytes(2, (C.c_uint64 * 2)(4000, 4000), 1, 48, 0, 1)
+    assert need > 0
+    ws = torch.full((1024,), 7.0, device="cuda")
+    dz = [torch.empty_like(v) for v in dy]
+    rc = ctx._L.slimdp_linear_epilogue_backward(ctx._h, 2, (C.c_uint64 * 2)(4000, 4000), 48, 0, binding._table(dy), 48, binding._table(z), 48, 4,
+                                                binding._table(dz), 48, None, 0, ws.data_ptr(), 64)
+    assert rc == binding.OK
+    _, db = ctx.linear_epilogue_backward(dy, z, "silu", dbias=[None, out])
+    _, dw, dbn = ctx.layer_norm_backward(dy, z, None, [v[:, 0].contiguous() for v in z], [v[:, 1].abs().contiguous() for v in z], dweight=[None, out.clone()], dbias=[None, None])
+    ctx.synchronize()
+    assert bool((ws == 7.0).all())
+    assert all(torch.equal(a, b) for a, b in zip(want[0], dz))
+    assert torch.equal(out, want[1][1]) and bool(dw[1].isfinite().all())
+
+
 # ---------------------------------------------------------------------------------------------------------------
 # distillation
 # ---------------------------------------------------------------------------------------------------------------
@@ -839,9 +860,14 @@ def test_refusals_of_the_c_entries(ctx):
         return L.slimdp_distill_loss(h, 1, n, V, dt, x, ldl, top, i, v, ldt, tau, w, loss, lse, d, ldd)
     for want, kw in [(INV, dict(V=0)), (RANGE, dict(V=binding.MAX_VOCAB + 1, ldl=1 << 25, ldd=1 << 25)), (RANGE, dict(top=1025, ldt=1025)), (INV, dict(i=None)), (INV, dict(v=None)),
                      (INV, dict(ldt=3)), (INV, dict(ldl=99)), (INV, dict(tau=0.0)), (INV, dict(tau=-1.0)), (INV, dict(tau=float("nan"))), (INV, dict(tau=float("inf"))),
-                     (INV, dict(tau=1e-45)), (INV, dict(d=a, ldd=101)), (INV, dict(x=None)), (INV, dict(w=odd))]:
+                     (INV, dict(tau=1e-45)), (INV, dict(tau=3e-39)), (INV, dict(d=a, ldd=101)), (INV, dict(x=None)), (INV, dict(w=odd))]:
         assert dist(**kw) == want, kw
+    assert norm(mean=o, rstd=o) == INV and back(rows=n, dw=vec, db=vec) == INV and dist(loss=vec, lse=vec) == INV
     two = (C.c_uint64 * 2)(4, 4)
+    # one worker's output over another's input: also where a worker's own would be allowed
+    cross, here = (C.c_void_p * 2)(buf.data_ptr(), keep.data_ptr()), (C.c_void_p * 2)(keep.data_ptr(), buf.data_ptr() + 4096)
+    assert L.slimdp_layer_norm(h, 2, two, 16, 0, cross, 16, None, None, 1e-5, here, 16, None, None) == INV
+    assert L.slimdp_linear_epilogue_backward(h, 2, two, 8, 0, cross, 8, cross, 8, 1, here, 8, None, 0, None, 0) == INV
     xs, ys = (C.c_void_p * 2)(buf.data_ptr(), buf.data_ptr()), (C.c_void_p * 2)(keep.data_ptr(), keep.data_ptr())
     assert L.slimdp_layer_norm(h, 2, two, 16, 0, xs, 16, None, None, 1e-5, ys, 16, None, None) == INV      # one output for two workers
     ctx.synchronize()
