@@ -168,14 +168,28 @@ def _u64arr(vals) -> "C.Array":
     return _array(C.c_uint64, max(1, len(vals)))(*vals)
 
 
-def _dtypes(torch) -> dict:
-    global _dtype_codes
-    if _dtype_codes is None:
-        _dtype_codes = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
-    return _dtype_codes
+def _types(torch) -> dict:
+    """Numbers of the element types: the library's, and 3 for int32 (lists of indices)."""
+    global _type_numbers
+    if _type_numbers is None:
+        _type_numbers = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16, torch.int32: 3}
+    return _type_numbers
 
 
-_dtype_codes = None
+def _tables():
+    """The compiled form of the checks below (None where it is not built: they then run as written)."""
+    global _helper
+    if _helper is False:
+        try:
+            from . import _tables as helper
+        except ImportError:
+            helper = None
+        _helper = helper
+    return _helper
+
+
+_type_numbers = None
+_helper = False
 
 
 def _seg_off(n: int, seg_off) -> "C.Array":
@@ -470,8 +484,8 @@ class SlimDP:
         if x[0].dim() != 2:
             raise ValueError(f"{who}: expected one two-dimensional tensor a worker")
         dtype = x[0].dtype
-        code = _dtypes(self._torch).get(dtype)
-        if code is None:
+        code = _types(self._torch).get(dtype, 3)
+        if code > BF16:
             raise ValueError(f"{who}: unsupported dtype {dtype}")
         return [v.shape[0] for v in x], x[0].shape[1], code, dtype
 
@@ -481,6 +495,12 @@ class SlimDP:
             return None, 0
         if len(ts) != len(rows):
             raise ValueError(f"{who}: {name} holds {len(ts)} tensors for {len(rows)} workers")
+        fast = _tables()
+        if fast is not None:
+            table = _array(C.c_void_p, len(ts))()
+            ld = fast.matrix(ts if type(ts) is list else list(ts), rows, cols, _types(self._torch)[dtype], self._index, C.addressof(table))
+            if ld >= 0:
+                return table, ld or cols
         ptrs, ld, device = [], -1, self._index
         for t, r in zip(ts, rows):                     # a handful of attributes a tensor: small calls wait for this loop
             if t.dtype is not dtype or t.shape != (r, cols) or t.get_device() != device:
@@ -505,6 +525,11 @@ class SlimDP:
             return None
         if len(ts) != len(sizes):
             raise ValueError(f"{who}: {name} holds {len(ts)} tensors for {len(sizes)} workers")
+        fast = _tables()
+        if fast is not None:
+            table = _array(C.c_void_p, len(ts))()
+            if fast.vectors(ts if type(ts) is list else list(ts), sizes, _types(self._torch)[dtype], self._index, C.addressof(table)) == 0:
+                return table
         ptrs, device = [], self._index
         for t, n in zip(ts, sizes):
             if t is None or (n == 0 and t.numel() == 0):

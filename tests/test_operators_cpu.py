@@ -65,7 +65,13 @@ class Host(binding.SlimDP):
         return make()
 
 
-def test_binding_refuses_what_does_not_fit():
+@pytest.mark.parametrize("compiled", [True, False])
+def test_binding_refuses_what_does_not_fit(monkeypatch, compiled):
+    """By the compiled checks, and as the binding spells them out."""
+    if compiled:
+        assert binding._tables() is not None, "the binding's helper is not built"
+    else:
+        monkeypatch.setattr(binding, "_helper", None)
     sd, Z = Host(), torch.zeros
     x, v = Z(4, 8), Z(8)
 
@@ -113,3 +119,20 @@ def test_binding_refuses_what_does_not_fit():
     refused(lambda: sd.distill_loss([x], [i], [Z(4, 2)]))
     refused(lambda: sd.distill_loss([x], [i], [Z(4, 6)[:, :3]]))                             # index and value at different distances
     refused(lambda: sd.distill_loss([x], [i], [t], row_weight=[Z(3)]))
+
+
+def test_compiled_tables_are_those_of_the_binding(monkeypatch):
+    sd, Z = Host(), torch.zeros
+    lists = [([Z(4, 16)[:, 3:11], Z(0, 8), Z(1, 8), Z(2, 16)[:, :8]], [4, 0, 1, 2], 8), ([Z(3, 1)], [3], 1), ((Z(5, 7), Z(5, 7)), [5, 5], 7)]
+    for ts, rows, cols in lists:
+        fast = sd._matrix("t", "x", ts, rows, cols, torch.float32)
+        with monkeypatch.context() as m:
+            m.setattr(binding, "_helper", None)
+            slow = sd._matrix("t", "x", ts, rows, cols, torch.float32)
+        assert list(fast[0]) == list(slow[0]) and fast[1] == slow[1]
+    vs = [Z(6)[1:5], None, Z(2, 2), Z(0)]
+    fast = sd._vectors("t", "v", vs, [4, 9, 4, 0], torch.float32)
+    with monkeypatch.context() as m:
+        m.setattr(binding, "_helper", None)
+        slow = sd._vectors("t", "v", vs, [4, 9, 4, 0], torch.float32)
+    assert list(fast) == list(slow)
