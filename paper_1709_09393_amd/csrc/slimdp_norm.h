@@ -410,8 +410,8 @@ struct ColumnArgs {
     int accumulate;
 };
 
-// NORM: out0 = sum dy * xh, out1 = sum dy.  Otherwise dz = dy * act'(z) and out1 = sum dz, from the values before they are rounded.
-template <class T, bool NORM, int ACT>
+// NT: streams pass the caches by.  NORM: out0 = sum dy * xh, out1 = sum dy.  Otherwise dz = dy * act'(z) and out1 = sum dz, from the values before they are rounded.
+template <class T, bool NORM, int ACT, int NT>
 __global__ __launch_bounds__(256) void k_column_grads(ColumnArgs a)
 {
     constexpr int V = Vec<T>::N, ARR = NORM ? 2 : 1;
@@ -428,29 +428,43 @@ __global__ __launch_bounds__(256) void k_column_grads(ColumnArgs a)
     float s0[V], s1[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) s0[i] = s1[i] = 0.0f;
-    if (c < cols)
-        for (uint32_t r = r0 + wave; r < r1; r += 4) {
-            float f[V], g[V];
-            unpack<T>(load_clip(pa + (size_t)r * a.lda, c, cols), f);
-            if (NORM) {
-                const float mean = static_cast<const float*>(a.mean.p[q])[r], rstd = static_cast<const float*>(a.rstd.p[q])[r];
-                unpack<T>(load_clip(pb + (size_t)r * a.ldb, c, cols), g);
+    auto one = [&](uint32_t r, raw4 va, raw4 vb) {
+        float f[V], g[V];
+        unpack<T>(va, f);
+        if (NORM) {
+            const float mean = static_cast<const float*>(a.mean.p[q])[r], rstd = static_cast<const float*>(a.rstd.p[q])[r];
+            unpack<T>(vb, g);
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    s0[i] = __builtin_fmaf(f[i], (g[i] - mean) * rstd, s0[i]);
-                    s1[i] += f[i];
-                }
-            } else {
-                if constexpr (ACT != ACT_NONE) {
-                    unpack<T>(load_clip(pb + (size_t)r * a.ldb, c, cols), g);
-#pragma unroll
-                    for (int i = 0; i < V; ++i) f[i] *= act_slope<ACT>(g[i]);
-                }
-                if (dz) store_clip(dz + (size_t)r * a.lddz, c, cols, pack<T>(f));
-#pragma unroll
-                for (int i = 0; i < V; ++i) s1[i] += f[i];
+            for (int i = 0; i < V; ++i) {
+                s0[i] = __builtin_fmaf(f[i], (g[i] - mean) * rstd, s0[i]);
+                s1[i] += f[i];
             }
+        } else {
+            if constexpr (ACT != ACT_NONE) {
+                unpack<T>(vb, g);
+#pragma unroll
+                for (int i = 0; i < V; ++i) f[i] *= act_slope<ACT>(g[i]);
+            }
+            if (dz) store_clip<T, NT>(dz + (size_t)r * a.lddz, c, cols, pack<T>(f));
+#pragma unroll
+            for (int i = 0; i < V; ++i) s1[i] += f[i];
         }
+    };
+    constexpr bool TWO = NORM || ACT != ACT_NONE;
+    if (c < cols) {
+        uint32_t r = r0 + wave;
+        for (; r + 4 < r1; r += 8) {             // two rows' vectors under way at a time
+            const raw4 a0 = load_clip<T, NT>(pa + (size_t)r * a.lda, c, cols), a1 = load_clip<T, NT>(pa + (size_t)(r + 4) * a.lda, c, cols);
+            const raw4 b0 = TWO ? load_clip<T, NT>(pb + (size_t)r * a.ldb, c, cols) : a0;
+            const raw4 b1 = TWO ? load_clip<T, NT>(pb + (size_t)(r + 4) * a.ldb, c, cols) : a1;
+            one(r, a0, b0);
+            one(r + 4, a1, b1);
+        }
+        if (r < r1) {
+            const raw4 a0 = load_clip<T, NT>(pa + (size_t)r * a.lda, c, cols);
+            one(r, a0, TWO ? load_clip<T, NT>(pb + (size_t)r * a.ldb, c, cols) : a0);
+        }
+    }
     if (wave) {
 #pragma unroll
         for (int i = 0; i < V; ++i) {

@@ -216,17 +216,23 @@ template <bool NORM> int column_grads(Call& c, ColumnArgs a, uint32_t dtype, int
     a.partial = sums && a.slabs > 1 ? static_cast<float*>(ws) : nullptr;
     with_type(dtype, [&](auto z) {
         typedef decltype(z) T;
-        auto launch = [&](auto kernel) {
+        const bool nt = c.bytes(a.cols, 3) > STREAM_BYTES;
+        auto launch = [&](auto kernel, auto kernel_nt) {
             c.launched("k_column_grads", [&] {
-                hipLaunchKernelGGL(kernel, dim3((uint32_t)ceil_div(a.cols, 64 * Vec<T>::N), a.slabs, c.W), dim3(256), 0, c.v.stream, a);
+                const dim3 grid((uint32_t)ceil_div(a.cols, 64 * Vec<T>::N), a.slabs, c.W);
+                if (nt) hipLaunchKernelGGL(kernel_nt, grid, dim3(256), 0, c.v.stream, a);
+                else hipLaunchKernelGGL(kernel, grid, dim3(256), 0, c.v.stream, a);
             });
         };
-        if constexpr (NORM) launch(k_column_grads<T, true, ACT_NONE>);
-        else if (act == ACT_RELU) launch(k_column_grads<T, false, ACT_RELU>);
-        else if (act == ACT_GELU) launch(k_column_grads<T, false, ACT_GELU>);
-        else if (act == ACT_GELU_TANH) launch(k_column_grads<T, false, ACT_GELU_TANH>);
-        else if (act == ACT_SILU) launch(k_column_grads<T, false, ACT_SILU>);
-        else launch(k_column_grads<T, false, ACT_NONE>);
+#define SLIMDP_COLUMNS(ACT) launch(k_column_grads<T, NORM, ACT, 0>, k_column_grads<T, NORM, ACT, 1>)
+        if (NORM || act == ACT_NONE) SLIMDP_COLUMNS(ACT_NONE);
+        else if constexpr (!NORM) {
+            if (act == ACT_RELU) SLIMDP_COLUMNS(ACT_RELU);
+            else if (act == ACT_GELU) SLIMDP_COLUMNS(ACT_GELU);
+            else if (act == ACT_GELU_TANH) SLIMDP_COLUMNS(ACT_GELU_TANH);
+            else SLIMDP_COLUMNS(ACT_SILU);
+        }
+#undef SLIMDP_COLUMNS
     });
     if (c.ok() && a.partial) {
         const ColumnSumArgs s{a.partial, a.out0, a.out1, c.tab, a.cols, a.slab, a.slabs, (uint32_t)ARR, a.accumulate};
