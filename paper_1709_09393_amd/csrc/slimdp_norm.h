@@ -395,7 +395,8 @@ __global__ __launch_bounds__(BT) void k_norm_back(NormBackArgs a, NormBackSums o
 }
 
 // ---------------------------------------------------------------------------------------
-// Sums over rows.  A block owns 64 vectors of consecutive columns and a slab of consecutive rows, its four waves every fourth row of it;
+// Sums over rows.  A block owns up to 64 vectors of consecutive columns (LX, as many as narrow matrices have) and a slab of consecutive
+// rows, its 256 / LX groups of threads every so many rows of it;
 // the slabs' partial sums meet in k_column_sums.  Which rows a slab holds depends on the sizes alone and every sum has a
 // fixed order: the same bits every time.
 // ---------------------------------------------------------------------------------------
@@ -411,14 +412,15 @@ struct ColumnArgs {
 };
 
 // NT: streams pass the caches by.  NORM: out0 = sum dy * xh, out1 = sum dy.  Otherwise dz = dy * act'(z) and out1 = sum dz, from the values before they are rounded.
-template <class T, bool NORM, int ACT, int NT>
+template <class T, bool NORM, int ACT, int LX, int NT>
 __global__ __launch_bounds__(256) void k_column_grads(ColumnArgs a)
 {
     constexpr int V = Vec<T>::N, ARR = NORM ? 2 : 1;
-    __shared__ float part[3][ARR][V][64];
+    constexpr uint32_t GROUPS = 256 / LX;
+    __shared__ float part[ARR][V][256];
     const uint32_t q = blockIdx.z, rows = a.rows.n[q], cols = a.cols;
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-    const uint32_t c = (blockIdx.x * 64 + lane) * V, slab = blockIdx.y;
+    const uint32_t lane = threadIdx.x % LX, group = threadIdx.x / LX;
+    const uint32_t c = (blockIdx.x * LX + lane) * V, slab = blockIdx.y;
     const uint32_t r0 = slab * a.slab;
     if (r0 >= rows && slab) return;              // the whole block; the first slab of an empty worker writes zeros
     const uint32_t r1 = min(rows, r0 + a.slab);
@@ -452,28 +454,26 @@ __global__ __launch_bounds__(256) void k_column_grads(ColumnArgs a)
     };
     constexpr bool TWO = NORM || ACT != ACT_NONE;
     if (c < cols) {
-        uint32_t r = r0 + wave;
-        for (; r + 4 < r1; r += 8) {             // two rows' vectors under way at a time
-            const raw4 a0 = load_clip<T, NT>(pa + (size_t)r * a.lda, c, cols), a1 = load_clip<T, NT>(pa + (size_t)(r + 4) * a.lda, c, cols);
+        uint32_t r = r0 + group;
+        for (; r + GROUPS < r1; r += 2 * GROUPS) {             // two rows' vectors under way at a time
+            const raw4 a0 = load_clip<T, NT>(pa + (size_t)r * a.lda, c, cols), a1 = load_clip<T, NT>(pa + (size_t)(r + GROUPS) * a.lda, c, cols);
             const raw4 b0 = TWO ? load_clip<T, NT>(pb + (size_t)r * a.ldb, c, cols) : a0;
-            const raw4 b1 = TWO ? load_clip<T, NT>(pb + (size_t)(r + 4) * a.ldb, c, cols) : a1;
+            const raw4 b1 = TWO ? load_clip<T, NT>(pb + (size_t)(r + GROUPS) * a.ldb, c, cols) : a1;
             one(r, a0, b0);
-            one(r + 4, a1, b1);
+            one(r + GROUPS, a1, b1);
         }
         if (r < r1) {
             const raw4 a0 = load_clip<T, NT>(pa + (size_t)r * a.lda, c, cols);
             one(r, a0, TWO ? load_clip<T, NT>(pb + (size_t)r * a.ldb, c, cols) : a0);
         }
     }
-    if (wave) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            if (NORM) part[wave - 1][ARR - 1][i][lane] = s0[i];
-            part[wave - 1][0][i][lane] = s1[i];
-        }
+    for (int i = 0; i < V; ++i) {
+        if (NORM) part[ARR - 1][i][threadIdx.x] = s0[i];
+        part[0][i][threadIdx.x] = s1[i];
     }
     __syncthreads();
-    if (wave == 0 && c < cols) {
+    if (group == 0 && c < cols) {
         float* p0 = NORM ? static_cast<float*>(a.out0.p[q]) : nullptr;
         float* p1 = static_cast<float*>(a.out1.p[q]);
         if (a.partial) {
@@ -485,9 +485,9 @@ __global__ __launch_bounds__(256) void k_column_grads(ColumnArgs a)
         for (int i = 0; i < V; ++i) {
             if (c + i >= cols) break;
 #pragma unroll
-            for (int w = 0; w < 3; ++w) {
-                if (NORM) s0[i] += part[w][ARR - 1][i][lane];
-                s1[i] += part[w][0][i][lane];
+            for (uint32_t g = 1; g < GROUPS; ++g) {
+                if (NORM) s0[i] += part[ARR - 1][i][g * LX + lane];
+                s1[i] += part[0][i][g * LX + lane];
             }
             if (NORM && p0) p0[c + i] = add ? p0[c + i] + s0[i] : s0[i];
             if (p1) p1[c + i] = add ? p1[c + i] + s1[i] : s1[i];
@@ -495,7 +495,8 @@ __global__ __launch_bounds__(256) void k_column_grads(ColumnArgs a)
     }
 }
 
-// The slabs' sums of column c, added in the order of the slabs: sixteen threads a column take every sixteenth slab, then their sums in order.
+// The slabs' sums of column c: SL threads a column (16, or 64 of many slabs) take every SL-th slab, eight asked for at a time; their sums meet
+// eight and eight.  The order goes by the number of slabs alone.  (With sixteen threads and one slab at a time the 1,024 slabs of 16,384 rows took as long as the rows.)
 struct ColumnSumArgs {
     const float* partial;
     OutTab out0, out1;
@@ -503,21 +504,38 @@ struct ColumnSumArgs {
     uint32_t cols, slab, slabs, arrays;   // slab 0: every worker has all the slabs
     int accumulate;
 };
-__global__ __launch_bounds__(256) void k_column_sums(ColumnSumArgs a)
+template <uint32_t SL>
+__global__ __launch_bounds__(16 * SL) void k_column_sums(ColumnSumArgs a)
 {
-    __shared__ float part[16][17];
+    __shared__ float part[SL][17];
     const uint32_t q = blockIdx.z, arr = blockIdx.y, tx = threadIdx.x & 15u, ty = threadIdx.x >> 4;
     const uint32_t c = blockIdx.x * 16 + tx;
     const uint32_t n = a.slab ? max(1u, (a.rows.n[q] + a.slab - 1) / a.slab) : a.slabs;
+    const float* from = a.partial + ((size_t)q * a.slabs * a.arrays + arr) * a.cols + c;
+    const size_t step = (size_t)a.arrays * a.cols;
     float s = 0.0f;
     if (c < a.cols)
-        for (uint32_t p = ty; p < n; p += 16) s += a.partial[(((size_t)q * a.slabs + p) * a.arrays + arr) * a.cols + c];
+        for (uint32_t p = ty; p < n; p += 8 * SL) {
+            float v[8];
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) v[i] = p + SL * i < n ? from[(p + SL * i) * step] : 0.0f;
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) s += v[i];
+        }
     part[ty][tx] = s;
+    __syncthreads();
+    if (ty < 8) {
+#pragma unroll
+        for (uint32_t i = 1; i < SL / 8; ++i) s += part[ty + 8 * i][tx];
+    }
+    __syncthreads();
+    if (ty < 8) part[ty][tx] = s;
     __syncthreads();
     if (ty == 0 && c < a.cols) {
         float* out = static_cast<float*>(arr == 0 && a.arrays == 2 ? a.out0.p[q] : a.out1.p[q]);
         if (!out) return;
-        for (int p = 1; p < 16; ++p) s += part[p][tx];
+#pragma unroll
+        for (uint32_t i = 1; i < 8; ++i) s += part[i][tx];
         out[c] = a.accumulate ? out[c] + s : s;
     }
 }

@@ -179,11 +179,19 @@ bool shape_ok(uint32_t n_workers, const uint64_t* rows)
     return n_workers && n_workers <= SLIMDP_MAX_WORKERS && rows && most_rows(n_workers, rows) <= SLIMDP_MAX_ROWS;
 }
 
-// Rows of a slab of the sums over rows: as many slabs as give the chip eight blocks a compute unit (of 256), of sixteen rows or more.
+// Vectors that a block of the sums over rows takes of a row.
+uint32_t column_lanes(uint64_t cols, size_t es)
+{
+    const uint64_t n = ceil_div(cols, 16 / es);
+    return n <= 8 ? 8 : n <= 16 ? 16 : n <= 32 ? 32 : 64;
+}
+// Rows of a slab of the sums over rows: as many slabs as give the chip eight blocks a compute unit (of 256), of four rows or more for
+// every group of a block's threads.
 uint64_t slab_rows(uint64_t most, uint32_t W, uint64_t cols, size_t es)
 {
-    const uint64_t across = ceil_div(cols, 64 * (16 / es)) * W;
-    const uint64_t slabs = std::max<uint64_t>(1, std::min<uint64_t>(2048 / across, ceil_div(most, 16)));
+    const uint32_t lx = column_lanes(cols, es);
+    const uint64_t across = ceil_div(cols, lx * (16 / es)) * W;
+    const uint64_t slabs = std::max<uint64_t>(1, std::min<uint64_t>(2048 / across, ceil_div(most, 4 * 256 / lx)));
     return std::max<uint64_t>(1, ceil_div(most, slabs));
 }
 uint64_t column_ws(uint64_t most, uint32_t W, uint64_t cols, size_t es, int arrays)
@@ -206,6 +214,15 @@ NormBackShape norm_back_shape(uint64_t most, uint32_t W, uint64_t cols, size_t e
     return {tpr, block, std::max<uint64_t>(1, std::min(fill, ceil_div(most, 4 * groups)))};
 }
 
+void column_sums(Call& c, const ColumnSumArgs& s)
+{
+    c.launched("k_column_sums", [&] {
+        const dim3 grid((uint32_t)ceil_div(s.cols, 16), s.arrays, c.W);
+        if (s.slabs <= 128) hipLaunchKernelGGL(k_column_sums<16>, grid, dim3(256), 0, c.v.stream, s);
+        else hipLaunchKernelGGL(k_column_sums<64>, grid, dim3(1024), 0, c.v.stream, s);
+    });
+}
+
 // ws: for the slabs' sums; nullptr where no sums are asked for.
 template <bool NORM> int column_grads(Call& c, ColumnArgs a, uint32_t dtype, int act, bool sums, void* ws)
 {
@@ -217,17 +234,25 @@ template <bool NORM> int column_grads(Call& c, ColumnArgs a, uint32_t dtype, int
     with_type(dtype, [&](auto z) {
         typedef decltype(z) T;
         const bool nt = c.bytes(a.cols, 3) > STREAM_BYTES;
+        const uint32_t lx = column_lanes(a.cols, c.esize);
         auto launch = [&](auto kernel, auto kernel_nt) {
             c.launched("k_column_grads", [&] {
-                const dim3 grid((uint32_t)ceil_div(a.cols, 64 * Vec<T>::N), a.slabs, c.W);
+                const dim3 grid((uint32_t)ceil_div(a.cols, lx * Vec<T>::N), a.slabs, c.W);
                 if (nt) hipLaunchKernelGGL(kernel_nt, grid, dim3(256), 0, c.v.stream, a);
                 else hipLaunchKernelGGL(kernel, grid, dim3(256), 0, c.v.stream, a);
             });
         };
-#define SLIMDP_COLUMNS(ACT) launch(k_column_grads<T, NORM, ACT, 0>, k_column_grads<T, NORM, ACT, 1>)
-        if (NORM || act == ACT_NONE) SLIMDP_COLUMNS(ACT_NONE);
-        else if constexpr (!NORM) {
-            if (act == ACT_RELU) SLIMDP_COLUMNS(ACT_RELU);
+#define SLIMDP_COLUMNS(ACT)                                                                                      \
+    do {                                                                                                         \
+        if (lx == 8) launch(k_column_grads<T, NORM, ACT, 8, 0>, k_column_grads<T, NORM, ACT, 8, 1>);             \
+        else if (lx == 16) launch(k_column_grads<T, NORM, ACT, 16, 0>, k_column_grads<T, NORM, ACT, 16, 1>);     \
+        else if (lx == 32) launch(k_column_grads<T, NORM, ACT, 32, 0>, k_column_grads<T, NORM, ACT, 32, 1>);     \
+        else launch(k_column_grads<T, NORM, ACT, 64, 0>, k_column_grads<T, NORM, ACT, 64, 1>);                   \
+    } while (0)
+        if constexpr (NORM) launch(k_column_grads<T, true, ACT_NONE, 64, 0>, k_column_grads<T, true, ACT_NONE, 64, 1>);      // long rows only
+        else {
+            if (act == ACT_NONE) SLIMDP_COLUMNS(ACT_NONE);
+            else if (act == ACT_RELU) SLIMDP_COLUMNS(ACT_RELU);
             else if (act == ACT_GELU) SLIMDP_COLUMNS(ACT_GELU);
             else if (act == ACT_GELU_TANH) SLIMDP_COLUMNS(ACT_GELU_TANH);
             else SLIMDP_COLUMNS(ACT_SILU);
@@ -235,10 +260,7 @@ template <bool NORM> int column_grads(Call& c, ColumnArgs a, uint32_t dtype, int
 #undef SLIMDP_COLUMNS
     });
     if (c.ok() && a.partial) {
-        const ColumnSumArgs s{a.partial, a.out0, a.out1, c.tab, a.cols, a.slab, a.slabs, (uint32_t)ARR, a.accumulate};
-        c.launched("k_column_sums", [&] {
-            hipLaunchKernelGGL(k_column_sums, dim3((uint32_t)ceil_div(a.cols, 16), ARR, c.W), dim3(256), 0, c.v.stream, s);
-        });
+        column_sums(c, ColumnSumArgs{a.partial, a.out0, a.out1, c.tab, a.cols, a.slab, a.slabs, (uint32_t)ARR, a.accumulate});
     }
     return c.rc;
 }
@@ -489,12 +511,7 @@ int slimdp_layer_norm_backward(slimdp_ctx* ctx, uint32_t n_workers, const uint64
             else SLIMDP_NORM_BACK(1024, 2, 1024);
 #undef SLIMDP_NORM_BACK
         });
-        if (c.ok() && o.partial) {
-            const ColumnSumArgs s{o.partial, o.dweight, o.dbias, c.tab, (uint32_t)cols, 0, (uint32_t)shape.blocks, 2, accumulate};
-            c.launched("k_column_sums", [&] {
-                hipLaunchKernelGGL(k_column_sums, dim3((uint32_t)ceil_div(cols, 16), 2, c.W), dim3(256), 0, c.v.stream, s);
-            });
-        }
+        if (c.ok() && o.partial) column_sums(c, ColumnSumArgs{o.partial, o.dweight, o.dbias, c.tab, (uint32_t)cols, 0, (uint32_t)shape.blocks, 2, accumulate});
         return c.rc;
     }
     if (sums) {      // before dx, which may overwrite dy or x
