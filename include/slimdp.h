@@ -319,7 +319,7 @@ int slimdp_pull(slimdp_ctx* ctx, const float* w, uint64_t core_epoch, uint32_t n
  *     w_local[q][i] <- fma(-eta, grad[q][i], w_local[q][i])
  *     delta[q][i]   <- grad[q][i]                      with SLIMDP_LOCAL_FIRST (first mini-batch after a communication)
  *     delta[q][i]   <- delta[q][i] + grad[q][i]        otherwise: the sum over the p mini-batches in binary32, in order
- * The gradient is an input (the library trains no network).  delta[q] is what slimdp_pack takes as g[q]; after the
+ * The gradient is an input (what makes it: the operators of LocalTrain below).  delta[q] is what slimdp_pack takes as g[q]; after the
  * push, slimdp_pull overwrites w_local[q] at the communication set (steps 4 and 5) and leaves the rest to diverge
  * from the global model, which is what the explorer is for (section 3.1).
  *   w_local, grad, delta [host tables, n_workers] of [dev, n], pairwise distinct per worker; eta finite. */
