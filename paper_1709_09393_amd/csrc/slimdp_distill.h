@@ -98,7 +98,7 @@ __global__ __launch_bounds__(BT) void k_distill(DistillArgs a)
                 if (at[k] != 0xFFFFFFFFu) atomicOr(a.status, STATUS_TEACHER);
                 at[k] = 0xFFFFFFFFu;
             }
-            vmax = fmaxf(vmax, mine[k]);
+            vmax = fmaxf(vmax, mine[k] == mine[k] ? mine[k] : INF);              // a NaN must not look like no entry
         }
         put(wave_max_f(vmax), slots[0]);
         __syncthreads();

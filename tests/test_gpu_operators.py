@@ -196,7 +196,7 @@ def test_layer_norm_backward_matches_the_formula(ctx, dtype, pad, shift):
         dy = [mk.normal(r, cols, t, 0.3) for r in rows]
         w = [mk.vec(cols, 0.3, 1.0) for _ in rows]
         mean = [v.double().mean(1).float() for v in x]
-        rstd = [(v.double().var(1, unbiased=False) + 1e-5).rsqrt().float() for v in x]
+        rstd = [((v.double() - v.double().mean(1, keepdim=True)).square().mean(1) + 1e-5).rsqrt().float() for v in x]
         dx = [mk.view(r, cols, t) for r in rows]
         old_w, old_b = [mk.vec(cols) for _ in rows], [mk.vec(cols) for _ in rows]
         dw, db = [v.clone() for v in old_w], [v.clone() for v in old_b]
@@ -573,6 +573,21 @@ def test_distill_rows_that_masks_leave_empty(ctx):
     close(d[0][5], rd[5], 1e-6, "dlogits of equal logits")      # q = 1 / V: a rounding of 1e38 would show in lse, not in q's size
 
 
+def test_distill_nan_goes_through(ctx):
+    mk = Maker(14)
+    for V in (300, 140000):
+        logits = mk.normal(4, V, torch.float32)
+        idx, val = teacher(mk, 4, V, 5, short=False)
+        val[0, 2] = float("nan")
+        val[1] = float("nan")                          # every entry
+        logits[2, 11] = float("nan")
+        loss, lse, d = ctx.distill_loss([logits], [idx], [val])
+        ctx.synchronize()
+        assert bool(loss[0][:3].isnan().all()) and bool(loss[0][3].isfinite())
+        assert bool(d[0][:3].isnan().any(1).all()) and bool(d[0][3].isfinite().all())
+        assert bool(lse[0][[0, 1, 3]].isfinite().all()) and bool(lse[0][2].isnan())
+
+
 def test_distill_all_logits_masked_and_no_teacher_at_all(ctx):
     logits = torch.full((2, 100), -float("inf"), device="cuda")
     idx = torch.full((2, 4), -1, dtype=torch.int32, device="cuda")
@@ -603,6 +618,45 @@ def test_distill_index_outside_the_vocabulary_is_reported_and_taken_as_none():
             assert torch.equal(a[0], b[0])
         sd.synchronize()                               # reported once
     sd.close()
+
+
+def test_rows_that_lie_further_apart_than_32_bits_reach(ctx):
+    """Inputs and outputs whose last rows begin behind 2^32 bytes and 2^31 elements: the same bits as of the rows side by side."""
+    R, ld, t = 40_000, 60_000, torch.bfloat16
+    mk = Maker(15)
+    big = [torch.empty((R, ld), dtype=t, device="cuda") for _ in range(2)]
+    x = mk.normal(R, 200, t)
+    far, out = big[0][:, 24:224], big[1][:, 7:207]
+    far.copy_(x)
+    w, b = mk.vec(200), mk.vec(200)
+    y, mean, rstd = ctx.layer_norm([x], [w], [b])
+    _, m2, r2 = ctx.layer_norm([far], [w], [b], y=[out])
+    ctx.synchronize()
+    assert torch.equal(out, y[0]) and torch.equal(m2[0], mean[0]) and torch.equal(r2[0], rstd[0])
+    dx, dw, _ = ctx.layer_norm_backward([x], y, [w], mean, rstd)
+    _, dw2, _ = ctx.layer_norm_backward([far], y, [w], mean, rstd, dx=[out])
+    ctx.synchronize()
+    assert torch.equal(out, dx[0]) and torch.equal(dw[0], dw2[0])
+    W = mk.normal(200, 200, t, 0.07)
+    z, _ = ctx.linear([x], [W], [b], "silu", residual=y)
+    ctx.linear([far], [W], [b], "silu", residual=y, y=[out])
+    ctx.synchronize()
+    assert torch.equal(out, z[0])
+    dx, dw = ctx.linear_backward([x], y, [W])
+    _, dw2 = ctx.linear_backward([far], y, [W], dx=[out])
+    ctx.synchronize()
+    assert torch.equal(out, dx[0]) and torch.equal(dw[0], dw2[0])
+    dz, db = ctx.linear_epilogue_backward([x], y, "gelu")
+    _, db2 = ctx.linear_epilogue_backward([far], y, "gelu", dz=[out])
+    ctx.synchronize()
+    assert torch.equal(out, dz[0]) and torch.equal(db[0], db2[0])
+    idx, val = teacher(mk, R, 200, 3)
+    l1, e1, d1 = ctx.distill_loss([x], [idx], [val])
+    l2, e2, _ = ctx.distill_loss([far], [idx], [val], dlogits=[out])
+    ctx.synchronize()
+    assert torch.equal(l1[0], l2[0]) and torch.equal(e1[0], e2[0]) and torch.equal(out, d1[0])
+    del big, far, out
+    torch.cuda.empty_cache()
 
 
 # ---------------------------------------------------------------------------------------------------------------
