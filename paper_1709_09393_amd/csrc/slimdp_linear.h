@@ -29,24 +29,25 @@ struct GemmArgs {
 // 16 bytes of either operand a lane: eight products' steps of sixteen-bit elements in one instruction, four of binary32 in one each.
 template <class T> struct Mma;
 template <> struct Mma<_Float16> {
-    static __device__ __forceinline__ f32x4 step(raw4 a, raw4 b, f32x4 c)
+    static constexpr int PARTS = 1;
+    static __device__ __forceinline__ f32x4 part(raw4 a, raw4 b, f32x4 c, int)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
     }
 };
 template <> struct Mma<__bf16> {
-    static __device__ __forceinline__ f32x4 step(raw4 a, raw4 b, f32x4 c)
+    static constexpr int PARTS = 1;
+    static __device__ __forceinline__ f32x4 part(raw4 a, raw4 b, f32x4 c, int)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     }
 };
 template <> struct Mma<float> {
-    // the four steps take the elements k, k + 4, k + 8, k + 12 of sixteen, the same ones of both operands
-    static __device__ __forceinline__ f32x4 step(raw4 a, raw4 b, f32x4 c)
+    // the four parts take the elements k, k + 4, k + 8, k + 12 of sixteen, the same ones of both operands
+    static constexpr int PARTS = 4;
+    static __device__ __forceinline__ f32x4 part(raw4 a, raw4 b, f32x4 c, int e)
     {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[i]), __uint_as_float(b[i]), c, 0, 0, 0);
-        return c;
+        return __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[e]), __uint_as_float(b[e]), c, 0, 0, 0);
     }
 };
 
@@ -73,38 +74,71 @@ template <class T> __device__ __forceinline__ void transpose(raw4 (&v)[Vec<T>::N
 
 // What becomes of four consecutive columns of one row of the sum.
 //   EPI 0: z = sum + bias, c = act(z) + residual, both in T      EPI 1: c = sum in T      EPI 2: c = sum in binary32, or c + sum
+template <class T> struct Four;
+template <> struct Four<float> { typedef uint32_t any __attribute__((ext_vector_type(4), aligned(4))); };
+template <> struct Four<_Float16> { typedef uint32_t any __attribute__((ext_vector_type(2), aligned(2))); };
+template <> struct Four<__bf16> { typedef uint32_t any __attribute__((ext_vector_type(2), aligned(2))); };
+template <class T> union FourPack { typename Four<T>::any r; T e[4]; };
+
+// Four consecutive elements, `left` of them inside the row.
+template <class T> __device__ __forceinline__ void load4(const T* p, uint32_t left, float f[4])
+{
+    if (left >= 4) {
+        FourPack<T> v;
+        v.r = *reinterpret_cast<const typename Four<T>::any*>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = (float)v.e[i];
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) f[i] = i < left ? (float)p[i] : 0.0f;
+    }
+}
+template <class T> __device__ __forceinline__ void store4(T* p, uint32_t left, const float f[4])
+{
+    if (left >= 4) {
+        FourPack<T> v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v.e[i] = (T)f[i];
+        *reinterpret_cast<typename Four<T>::any*>(p) = v.r;
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+            if (i < left) p[i] = (T)f[i];
+    }
+}
+
 template <class T, int EPI>
 __device__ __forceinline__ void epilogue4(const GemmArgs& a, uint32_t q, uint32_t m, uint32_t n, uint32_t N, const float s[4])
 {
-    float v[4] = {s[0], s[1], s[2], s[3]};
-    const bool full = n + 4 <= N;
+    const uint32_t left = N - n;
+    float v[4] = {s[0], s[1], s[2], s[3]}, x[4];
     if constexpr (EPI == 2) {
         float* c = static_cast<float*>(a.c.p[q]) + (size_t)m * a.ldc + n;
+        if (a.accumulate) {
+            load4(c, left, x);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (full || n + i < N) c[i] = a.accumulate ? c[i] + v[i] : v[i];
+            for (int i = 0; i < 4; ++i) v[i] += x[i];
+        }
+        store4(c, left, v);
     } else {
         if constexpr (EPI == 0) {
             const float* bias = static_cast<const float*>(a.bias.p[q]);
             T* z = static_cast<T*>(a.z.p[q]);
             const T* res = static_cast<const T*>(a.residual.p[q]);
+            if (bias) {
+                load4(bias + n, left, x);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (!full && n + i >= N) break;
-                if (bias) v[i] += bias[n + i];
-                if (z) z[(size_t)m * a.ldz + n + i] = (T)v[i];
+                for (int i = 0; i < 4; ++i) v[i] += x[i];
             }
+            if (z) store4(z + (size_t)m * a.ldz + n, left, v);
             act_values(v, a.act);
+            if (res) {
+                load4(res + (size_t)m * a.ldr + n, left, x);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (!full && n + i >= N) break;
-                if (res) v[i] += (float)res[(size_t)m * a.ldr + n + i];
+                for (int i = 0; i < 4; ++i) v[i] += x[i];
             }
         }
-        T* c = static_cast<T*>(a.c.p[q]) + (size_t)m * a.ldc + n;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (full || n + i < N) c[i] = (T)v[i];
+        store4(static_cast<T*>(a.c.p[q]) + (size_t)m * a.ldc + n, left, v);
     }
 }
 
@@ -112,9 +146,10 @@ __device__ __forceinline__ void epilogue4(const GemmArgs& a, uint32_t q, uint32_
 // pieces are loaded into registers while this one's are multiplied from shared memory; there either operand lies with k running,
 // 128 bytes a row, its eight vectors exchanged by the row's number so that the sixteen rows that a read touches meet
 // different banks.  Operands with rows of k are turned over in registers on the way.  Any size, stride and alignment: what lies
-// outside reads as zero.  S = 64 where 128 would leave compute units without a block.
+// outside reads as zero.  S = 64 where 128 would leave compute units without a block; such blocks wait for their loads, and have two
+// steps' under way.  NARROW: rows shorter than a vector, element by element.
 // grid (tiles, 1, workers * splits)
-template <class T, bool AK, bool BK_, int EPI, uint32_t S>
+template <class T, bool AK, bool BK_, int EPI, uint32_t S, bool NARROW>
 __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
 {
     constexpr uint32_t V = Vec<T>::N, BK = 8 * V, F = S / 32, RUN = S / 32;
@@ -131,17 +166,17 @@ __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
     // one operand's pieces of a step: RUN vectors a thread with k running, one square of V x V elements otherwise
     constexpr uint32_t SQ = S / V * 8;                             // squares of a tile
     constexpr int RA = AK ? (int)V : (int)RUN, RB = BK_ ? (int)V : (int)RUN;
-    raw4 ra[RA], rb[RB];
+    constexpr uint32_t DEPTH = S == 64 && !NARROW ? 2 : 1;
+    raw4 ra[DEPTH][RA], rb[DEPTH][RB];
     // Every load is made, from a place inside the matrix (the last row or vector in place of what lies outside), and what does not belong is
     // cleared when it is put into the LDS: a load behind a condition of its own waits for the ones before it (2048 x 4096 x 4096 bf16 with
-    // rows of k for either operand 368 us).  Matrices narrower than a vector are read element by element.
-    const bool narrow = (AK ? M : Kall) < V || (BK_ ? N : Kall) < V;
+    // rows of k for either operand 368 us).
     auto load = [&](auto krows, const T* P, uint64_t ld, uint32_t x0, uint32_t X, uint32_t kb, uint32_t tt, auto& reg) {
         if constexpr (!decltype(krows)::value) {
 #pragma unroll
             for (uint32_t i = 0; i < RUN; ++i) {
                 const uint32_t x = x0 + (t >> 3) + 32u * i, k = kb + (t & 7u) * V;
-                if (narrow) reg[i] = x < X && k < K ? load_clip(P + (size_t)x * ld, k, K) : raw4{0, 0, 0, 0};
+                if constexpr (NARROW) reg[i] = x < X && k < K ? load_clip(P + (size_t)x * ld, k, K) : raw4{0, 0, 0, 0};
                 else reg[i] = load_raw<T>(P + (size_t)min(x, X - 1) * ld + min(k, Kall - V));
             }
         } else {
@@ -149,7 +184,7 @@ __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
             const uint32_t x = x0 + (tt >> 3) * V, kr = kb + (tt & 7u) * V;        // eight lanes: a whole row of the LDS to write
 #pragma unroll
             for (uint32_t i = 0; i < V; ++i) {
-                if (narrow) reg[i] = x < X && kr + i < K ? load_clip(P + (size_t)(kr + i) * ld, x, X) : raw4{0, 0, 0, 0};
+                if constexpr (NARROW) reg[i] = x < X && kr + i < K ? load_clip(P + (size_t)(kr + i) * ld, x, X) : raw4{0, 0, 0, 0};
                 else reg[i] = load_raw<T>(P + (size_t)min(kr + i, K - 1) * ld + min(x, X - V));
             }
         }
@@ -160,7 +195,7 @@ __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
 #pragma unroll
             for (uint32_t i = 0; i < RUN; ++i) {
                 const uint32_t x = (t >> 3) + 32u * i;
-                if (!narrow) {
+                if constexpr (!NARROW) {
                     if (k < K && k + V > K) reg[i] = move_down<T>(reg[i], k + V - K);
                     if (k >= K || x0 + x >= X) reg[i] = raw4{0, 0, 0, 0};
                 }
@@ -168,7 +203,7 @@ __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
             }
         } else if (tt < SQ) {
             const uint32_t x = (tt >> 3) * V, ck = tt & 7u, kr = kb + ck * V;
-            if (!narrow) {
+            if constexpr (!NARROW) {
                 const uint32_t end = x0 + x + V;
                 if (end > X) {
 #pragma unroll
@@ -194,19 +229,16 @@ __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
     for (uint32_t i = 0; i < F; ++i)
 #pragma unroll
         for (uint32_t j = 0; j < F; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (k0 < K) {
-        load(ak_t{}, A, a.lda, m0, M, k0, ta, ra);
-        load(bk_t{}, B, a.ldb, n0, N, k0, tb, rb);
-    }
-    for (uint32_t kb = k0; kb < K; kb += BK) {
+    auto load_step = [&](uint32_t kb, uint32_t d) {
+        load(ak_t{}, A, a.lda, m0, M, kb, ta, ra[d]);
+        load(bk_t{}, B, a.ldb, n0, N, kb, tb, rb[d]);
+    };
+    auto step = [&](uint32_t kb, uint32_t d) {
         __syncthreads();
-        put(ak_t{}, sa, m0, M, kb, ta, ra);
-        put(bk_t{}, sb, n0, N, kb, tb, rb);
+        put(ak_t{}, sa, m0, M, kb, ta, ra[d]);
+        put(bk_t{}, sb, n0, N, kb, tb, rb[d]);
         __syncthreads();
-        if (kb + BK < K) {
-            load(ak_t{}, A, a.lda, m0, M, kb + BK, ta, ra);
-            load(bk_t{}, B, a.ldb, n0, N, kb + BK, tb, rb);
-        }
+        if (kb + DEPTH * BK < K) load_step(kb + DEPTH * BK, d);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             raw4 fa[F], fb[F];
@@ -219,10 +251,21 @@ __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
             }
             // B first: a lane then holds four consecutive columns of one row of C
 #pragma unroll
-            for (uint32_t i = 0; i < F; ++i)
+            for (int e = 0; e < Mma<T>::PARTS; ++e)
 #pragma unroll
-                for (uint32_t j = 0; j < F; ++j) acc[i][j] = Mma<T>::step(fb[j], fa[i], acc[i][j]);
+                for (uint32_t i = 0; i < F; ++i)
+#pragma unroll
+                    for (uint32_t j = 0; j < F; ++j) acc[i][j] = Mma<T>::part(fb[j], fa[i], acc[i][j], e);
         }
+    };
+    if (k0 < K) {
+#pragma unroll
+        for (uint32_t d = 0; d < DEPTH; ++d)
+            if (k0 + d * BK < K) load_step(k0 + d * BK, d);
+        for (uint32_t kb = k0; kb < K; kb += DEPTH * BK)
+#pragma unroll
+            for (uint32_t d = 0; d < DEPTH; ++d)
+                if (kb + d * BK < K) step(kb + d * BK, d);
     }
 #pragma unroll
     for (uint32_t i = 0; i < F; ++i) {
@@ -235,10 +278,7 @@ __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
             const float s[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
             if (a.splits == 1) epilogue4<T, EPI>(a, q, m, n, N, s);
             else {
-                float* p = a.partial + (((size_t)q * a.splits + split) * a.M + m) * N + n;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (n + e < N) p[e] = s[e];
+                store4(a.partial + (((size_t)q * a.splits + split) * a.M + m) * N + n, N - n, s);
             }
         }
     }
@@ -279,7 +319,9 @@ __global__ __launch_bounds__(512) void k_gemm_few(GemmArgs a)
 #pragma unroll
         for (uint32_t i = 0; i < AHEAD; ++i)
 #pragma unroll
-            for (int f = 0; f < MF; ++f) acc[f] = Mma<T>::step(vb[i], va[i][f], acc[f]);
+            for (int e = 0; e < Mma<T>::PARTS; ++e)
+#pragma unroll
+                for (int f = 0; f < MF; ++f) acc[f] = Mma<T>::part(vb[i], va[i][f], acc[f], e);
     }
 #pragma unroll
     for (int f = 0; f < MF; ++f) meet[wave][f][lane] = acc[f];
@@ -304,16 +346,10 @@ __global__ __launch_bounds__(256) void k_gemm_join(GemmArgs a)
     for (uint32_t m = blockIdx.y; m < M; m += gridDim.y) {
         float s[4] = {0.f, 0.f, 0.f, 0.f};
         for (uint32_t p = 0; p < a.splits; ++p) {
-            const float* src = a.partial + (((size_t)q * a.splits + p) * a.M + m) * N + n;
-            if (n + 4 <= N) {
-                const raw4 v = load_raw<float>(src);
+            float x[4];
+            load4(a.partial + (((size_t)q * a.splits + p) * a.M + m) * N + n, N - n, x);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[e] += __uint_as_float(v[e]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (n + e < N) s[e] += src[e];
-            }
+            for (int e = 0; e < 4; ++e) s[e] += x[e];
         }
         epilogue4<T, EPI>(a, q, m, n, N, s);
     }

@@ -280,8 +280,8 @@ struct Product {
     uint64_t tiles(uint32_t t) const { return ceil_div(M, t) * ceil_div(N, t); }
     // What a cut takes, as measured: `slots` blocks run at a time over the 256 compute units, `step` us for a step of all of them (less
     // where there is one block to a unit at most), `ends` us to begin and to write, and where the sum is cut the pieces' way to memory and back at
-    // 4 TB/s.  Products of 8192 x 8192 x 8192 and 8 x 2048 x 4096 x 4096, bf16: 1.45 us a step with 256 x 256, 0.95 with two of 128 x 128;
-    // through registers 1.9, binary32 3.6; a quarter of that and four blocks with 64 x 64.
+    // 4 TB/s.  Products of 8192 x 8192 x 8192 and 8 x 2048 x 4096 x 4096, bf16: 1.45 us a step with 256 x 256, 0.95 with two of 128 x 128.
+    // Through registers, binary32: 3.6 with two of 128 x 128, 2.0 with four of 64 x 64.
     struct Kernel { uint32_t tile, slots; double step, alone, ends; };
     Cut cut(const Kernel& k, uint64_t want) const
     {
@@ -304,11 +304,12 @@ struct Product {
     }
     // by copies into the LDS: sixteen-bit types
     Cut copies() const { return best({256, 256, 1.45, 1.45, 12.0}, {128, 512, 0.95, 0.65, 8.0}); }
-    // through registers: any layout
+    // through registers: binary32; and sixteen-bit types that cannot be copied, and rows shorter than a vector, element by element with 64 x 64
+    bool narrow() const { return es == 2 || std::min(N, rows_of_k ? M : K) < 4; }
     Cut registers() const
     {
-        const double f = es == 4 ? 3.6 : 1.9;
-        return best({128, 512, f, 0.6 * f, 8.0}, {64, 1024, 0.55 * f, 0.2 * f, 6.0});
+        const Kernel small = {64, 1024, 2.0, 0.7, 6.0};
+        return narrow() ? best(small, small) : best({128, 512, 3.6, 2.2, 8.0}, small);
     }
     bool few() const { return !rows_of_k && M <= 64; }
     static uint64_t bytes(const Cut& c, const Product& p) { return c.splits > 1 ? p.W * c.splits * p.M * p.N * 4 : 0; }
@@ -370,11 +371,16 @@ template <bool AK, bool BK, int EPI> int product(Call& c, GemmArgs a, const Prod
             else if (stage == 1 && cut.tile == 256) launch(k_gemm_tiles<T, AK, BK, EPI, 256, 256, 2, 2, 1, false>);
             else if (stage == 1) launch(k_gemm_tiles<T, AK, BK, EPI, 128, 128, 2, 2, 2, false>);
         }
-        if (stage == 2)
-            c.launched("k_gemm", [&] {
-                if (cut.tile == 128) hipLaunchKernelGGL((k_gemm<T, AK, BK, EPI, 128>), grid, dim3(256), 0, c.v.stream, a);
-                else hipLaunchKernelGGL((k_gemm<T, AK, BK, EPI, 64>), grid, dim3(256), 0, c.v.stream, a);
-            });
+        if (stage == 2) {
+            auto launch = [&](auto kernel) {
+                c.launched("k_gemm", [&] { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, c.v.stream, a); });
+            };
+            if (p.narrow()) launch(k_gemm<T, AK, BK, EPI, 64, true>);
+            else if constexpr (sizeof(T) == 4) {
+                if (cut.tile == 128) launch(k_gemm<T, AK, BK, EPI, 128, false>);
+                else launch(k_gemm<T, AK, BK, EPI, 64, false>);
+            }
+        }
         if (c.ok() && a.splits > 1)
             c.launched("k_gemm_join", [&] {
                 hipLaunchKernelGGL((k_gemm_join<T, EPI>), dim3((uint32_t)ceil_div(p.N, 1024), (uint32_t)std::min<uint64_t>(p.M, 1024), c.W),
