@@ -929,3 +929,38 @@ def test_refusals_of_the_c_entries(ctx):
     zero = (C.c_uint64 * 1)(0)
     assert norm(rows=zero, x=tab(None), y=tab(None)) == OKAY and norm() == OKAY
     ctx.synchronize()
+
+
+def check_products(ctx, mk, R, K, N, t, what):
+    x, w, dz, res = mk.normal(R, K, t), mk.normal(N, K, t, 0.03), mk.normal(R, N, t, 0.1), mk.normal(R, N, t)
+    b, old = mk.vec(N), mk.vec(N * K).view(N, K)
+    y, _ = ctx.linear([x], [w], [b], "none", [res])
+    dx, dw = ctx.linear_backward([dz], [x], [w])
+    add = [old.clone()]
+    ctx.linear_backward([dz], [x], None, dweight=add, want_dx=False, accumulate=True)
+    ctx.synchronize()
+    xd, wd, zd = x.double(), w.double(), dz.double()
+    # two additions behind the sum, of bias and residual, each rounded once to binary32; one behind the weight's gradient
+    ref, e = xd @ wd.t(), 1.01 * steps(K, t) * F * (xd.abs() @ wd.abs().t())
+    one, two = ref + b.double(), ref + b.double() + res.double()
+    close(y[0], two, u(t) * two.abs() + 1.01 * (e + F * (one.abs() + two.abs())) + tiny(t), what + " y")
+    ref = zd @ wd
+    close(dx[0], ref, u(t) * ref.abs() + 1.01 * steps(N, t) * F * (zd.abs() @ wd.abs()) + tiny(t), what + " dx")
+    ref, e = zd.t() @ xd, 1.01 * steps(R, t) * F * (zd.abs().t() @ xd.abs()) + 1e-30
+    close(dw[0], ref, F * ref.abs() + e, what + " dweight")
+    both = ref + old.double()
+    close(add[0], both, 1.01 * e + F * (ref.abs() + both.abs()), what + " dweight added")
+    mk.check_gaps()
+
+
+@pytest.mark.parametrize("R,K,N,pad,shift", [(2100, 1032, 2312, 0, 0), (2101, 1033, 2311, 3, 1), (1, 2001, 3005, 0, 0), (3, 2050, 4001, 1, 3), (2, 5, 4, 0, 0),
+                                             (640, 3, 2000, 0, 0), (5000, 2000, 3, 0, 1), (70, 4, 4100, 0, 0), (65, 6000, 66, 0, 0)])
+def test_products_in_binary32_of_every_tile(ctx, R, K, N, pad, shift):
+    """Large tiles and small ones, sums in pieces and whole, one to three rows, rows shorter than four elements; every element."""
+    check_products(ctx, Maker(31, pad, shift), R, K, N, torch.float32, f"{R} {K} {N}")
+
+
+def test_products_with_rows_far_apart(ctx):
+    """Distances between rows that no 32-bit offset of a tile holds."""
+    for t in (torch.bfloat16, torch.float16):
+        check_products(ctx, Maker(32, (1 << 21) + 5, 1), 67, 75, 70, t, str(t))
