@@ -286,16 +286,19 @@ __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
 
 // Few rows (up to 16 * MF): the second operand's bytes are all there is to wait for.  It goes from memory to registers as the instructions
 // take it (16 rows, four vectors of each at a time), every element once; a block has 16 of its rows and its eight waves a share of k
-// each, whose sums meet in the LDS in the order of the waves.  A wave asks for eight turns' vectors before it uses the first.
+// each, whose sums meet in the LDS in the order of the waves.  A wave has four to eight steps' vectors under way,
+// the number that leaves the fewest places empty in its share (four of 64 rows: more do not fit the registers), and asks for all of them
+// without a condition, from a place inside the row: loads behind a condition each took 57 us instead of 40 at 8 x 50 x 1024 x 4096 bf16,
+// 25.8 instead of 18.6 at 4 x 33 x 1000 x 4000, 58 instead of 45 at 64 x 4096 x 4096 binary32.  4 x 8 x 8192 x 8192 bf16 122 us (4.4 TB/s).
 // grid (ceil(N / 16), 1, workers)
 template <class T, int MF, int EPI>
 __global__ __launch_bounds__(512) void k_gemm_few(GemmArgs a)
 {
-    constexpr uint32_t V = Vec<T>::N, STEP = 4 * V, AHEAD = 8;
+    constexpr uint32_t V = Vec<T>::N, STEP = 4 * V;
     __shared__ f32x4 meet[8][MF][64];
     const uint32_t q = blockIdx.z, M = a.rows.n[q], N = a.N, K = a.K, n0 = blockIdx.x * 16;
     if (M == 0) return;
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, row = lane & 15u, part = (lane >> 4) * V;
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 15u, part = (lane >> 4) * V;
     const T* A = static_cast<const T*>(a.a.p[q]);
     const T* B = static_cast<const T*>(a.b.p[q]) + (size_t)min(n0 + row, N - 1) * a.ldb;        // rows outside: another's, not kept
     const uint32_t steps = (K + STEP - 1) / STEP, share = (steps + 7) / 8;
@@ -303,25 +306,61 @@ __global__ __launch_bounds__(512) void k_gemm_few(GemmArgs a)
     f32x4 acc[MF];
 #pragma unroll
     for (int f = 0; f < MF; ++f) acc[f] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (uint32_t s = s0; s < s1; s += AHEAD) {
-        raw4 vb[AHEAD], va[AHEAD][MF];
+    auto row_of_a = [&](int f) { return A + (size_t)min((uint32_t)f * 16 + row, M - 1) * a.lda; };
+    auto multiply = [&](raw4 vb, const raw4 (&va)[MF]) {
 #pragma unroll
-        for (uint32_t i = 0; i < AHEAD; ++i) {
-            const uint32_t k = (s + i) * STEP + part;
-            const bool in = s + i < s1 && k < K;
-            vb[i] = in ? load_clip<T, 1>(B, k, K) : raw4{0, 0, 0, 0};
+        for (int e = 0; e < Mma<T>::PARTS; ++e)
 #pragma unroll
-            for (int f = 0; f < MF; ++f) {
-                const uint32_t m = f * 16 + row;
-                va[i][f] = in && m < M ? load_clip(A + (size_t)m * a.lda, k, K) : raw4{0, 0, 0, 0};
+            for (int f = 0; f < MF; ++f) acc[f] = Mma<T>::part(vb, va[f], acc[f], e);
+    };
+    auto run = [&](auto ahead) {
+        constexpr uint32_t D = decltype(ahead)::value;
+        raw4 vb[D], va[D][MF];
+        auto ask = [&](uint32_t s, uint32_t i) {
+            const uint32_t k = min(min(s, s1 - 1) * STEP + part, K - V);
+            vb[i] = load_raw<T, 1>(B + k);
+#pragma unroll
+            for (int f = 0; f < MF; ++f) va[i][f] = load_raw<T>(row_of_a(f) + k);
+        };
+        auto use = [&](uint32_t s, uint32_t i) {
+            if ((s + 1) * STEP > K) {                                                            // the last step: what lies behind the rows' ends
+                const uint32_t k = s * STEP + part;
+                auto cut = [&](raw4& v) {
+                    if (k < K && k + V > K) v = move_down<T>(v, k + V - K);
+                    if (k >= K) v = raw4{0, 0, 0, 0};
+                };
+                cut(vb[i]);
+#pragma unroll
+                for (int f = 0; f < MF; ++f) cut(va[i][f]);
             }
+            multiply(vb[i], va[i]);
+        };
+#pragma unroll
+        for (uint32_t i = 0; i < D; ++i) ask(s0 + i, i);
+        uint32_t s = s0;
+        for (; s + D < s1; s += D)
+#pragma unroll
+            for (uint32_t i = 0; i < D; ++i) {
+                multiply(vb[i], va[i]);                                                          // never the last step
+                ask(s + D + i, i);
+            }
+#pragma unroll
+        for (uint32_t i = 0; i < D; ++i)
+            if (s + i < s1) use(s + i, i);
+    };
+    if (K < V) {
+        if (wave == 0) {
+            raw4 va[MF];
+#pragma unroll
+            for (int f = 0; f < MF; ++f) va[f] = part < K ? load_clip(row_of_a(f), part, K) : raw4{0, 0, 0, 0};
+            multiply(part < K ? load_clip(B, part, K) : raw4{0, 0, 0, 0}, va);
         }
-#pragma unroll
-        for (uint32_t i = 0; i < AHEAD; ++i)
-#pragma unroll
-            for (int e = 0; e < Mma<T>::PARTS; ++e)
-#pragma unroll
-                for (int f = 0; f < MF; ++f) acc[f] = Mma<T>::part(vb[i], va[i][f], acc[f], e);
+    } else if (s0 < s1) {
+        if (MF == 4 || share <= 4) run(std::integral_constant<uint32_t, 4>{});
+        else if constexpr (MF < 4) {
+            if ((share + 4) / 5 * 5 < (share + 7) / 8 * 8) run(std::integral_constant<uint32_t, 5>{});
+            else run(std::integral_constant<uint32_t, 8>{});
+        }
     }
 #pragma unroll
     for (int f = 0; f < MF; ++f) meet[wave][f][lane] = acc[f];

@@ -964,3 +964,11 @@ def test_products_with_rows_far_apart(ctx):
     """Distances between rows that no 32-bit offset of a tile holds."""
     for t in (torch.bfloat16, torch.float16):
         check_products(ctx, Maker(32, (1 << 21) + 5, 1), 67, 75, 70, t, str(t))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("R", [1, 17, 40, 64])
+def test_few_rows_with_every_share_of_a_wave(ctx, dtype, R):
+    """Rows shorter than a vector, waves without a share, with one to several turns of steps, and ends inside a vector."""
+    for pad, shift, K in ((0, 0, 3), (1, 1, 9), (0, 0, 33), (3, 1, 130), (0, 0, 999), (8, 8, 1280), (5, 3, 1290), (0, 0, 2049), (0, 0, 2600), (1, 0, 4111)):
+        check_products(ctx, Maker(33, pad, shift), R, K, 1040, TYPES[dtype], f"{dtype} {R} {K}")
