@@ -517,6 +517,8 @@ class SlimDP:
                     raise ValueError(f"{who}: rows of {name}[{len(ptrs)}] are {step} elements apart, expected {max(ld, cols)}")
                 ld = step
             ptrs.append(t.data_ptr())
+            if not ptrs[-1] and cols:
+                raise ValueError(f"{who}: {name}[{len(ptrs) - 1}] has no memory")
         return _array(C.c_void_p, len(ptrs))(*ptrs), max(ld, cols)
 
     def _vectors(self, who: str, name: str, ts, sizes, dtype):
@@ -539,6 +541,8 @@ class SlimDP:
                 raise ValueError(f"{who}: {name}[{len(ptrs)}] is {tuple(t.shape)} {t.dtype} on {t.device}, "
                                  f"expected {n} consecutive {dtype} on {self.device}")
             ptrs.append(t.data_ptr())
+            if not ptrs[-1] and n:
+                raise ValueError(f"{who}: {name}[{len(ptrs) - 1}] has no memory")
         return _array(C.c_void_p, len(ptrs))(*ptrs)
 
     def _new(self, make):
