@@ -26,7 +26,8 @@ struct DistillArgs {
 // the gradient's as they leave, and neither waits for the other's memory.  HELD = 0: rows that no block holds, read twice, and calls that ask for no
 // gradient (nothing is kept then: 128,000 columns of bf16, 4,096 rows: 192 us instead of 294).  NT: streams pass the caches by.
 // Exponentials are powers of two of (x - largest) * (log2 e / tau): the difference first, so that logits far from zero (a mask of the
-// type's lowest value over a whole row among them) lose nothing to the product's rounding.
+// type's lowest value over a whole row among them) lose nothing to the product's rounding, and the teacher's likewise: a value whose quotient
+// by a temperature below 1 is beyond the type's range is still a value.
 //
 // The teacher's entries are subtracted by the threads that own their places: every thread has a list of the entries in its vectors.
 // An entry that appears twice counts twice: the first of equal indices carries the sum, added in the order of the entries, and
@@ -92,7 +93,7 @@ __global__ __launch_bounds__(BT) void k_distill(DistillArgs a)
             if (j >= top) continue;
             at[k] = index[(size_t)r * a.ldt + j];
             if (at[k] < vocab) {
-                mine[k] = value[(size_t)r * a.ldt + j] * inv_tau;
+                mine[k] = value[(size_t)r * a.ldt + j];
                 logit[k] = (float)row[at[k]];
             } else {
                 if (at[k] != 0xFFFFFFFFu) atomicOr(a.status, STATUS_TEACHER);
@@ -107,7 +108,10 @@ __global__ __launch_bounds__(BT) void k_distill(DistillArgs a)
         float mass = 0.0f;
 #pragma unroll
         for (int k = 0; k < MINE; ++k)
-            if (live && at[k] != 0xFFFFFFFFu) mass += expf(mine[k] - vmax);
+            if (live && at[k] != 0xFFFFFFFFu) {
+                mine[k] = (mine[k] - vmax) / a.tau;
+                mass += expf(mine[k]);
+            }
         put(wave_sum_f(mass), slots[1]);
         __syncthreads();
         const float log_mass = logf(sum_of(slots[1]));
@@ -115,7 +119,7 @@ __global__ __launch_bounds__(BT) void k_distill(DistillArgs a)
         for (int k = 0; k < MINE; ++k) {
             const uint32_t j = k * BT + t;
             if (j >= top) continue;
-            mine[k] = live ? mine[k] - vmax - log_mass : -INF;                 // log p
+            mine[k] = live ? mine[k] - log_mass : -INF;                        // log p
             ti[j] = at[k];
             tp[j] = at[k] != 0xFFFFFFFFu ? expf(mine[k]) : 0.0f;
             if (live && dlogits && at[k] != 0xFFFFFFFFu) {

@@ -573,6 +573,36 @@ def test_distill_rows_that_masks_leave_empty(ctx):
     close(d[0][5], rd[5], 1e-6, "dlogits of equal logits")      # q = 1 / V: a rounding of 1e38 would show in lse, not in q's size
 
 
+@pytest.mark.parametrize("V,top", [(300, 4), (300, 400), (140000, 4)])
+def test_distill_teacher_values_far_from_zero(ctx, V, top):
+    """p depends on the differences of the values alone: far values whose quotients by the temperature overflow, or lose the difference."""
+    tau, mk = 0.7, Maker(16)
+    logits = mk.normal(6, V, torch.float32)
+    idx = torch.full((6, top), -1, dtype=torch.int32, device="cuda")
+    val = torch.zeros((6, top), device="cuda")
+    idx[:, :4] = torch.tensor([7, 100, 299, 1], dtype=torch.int32)
+    val[0, :4] = torch.tensor([3e38, 2e38, -3e38, 1.0])
+    val[1, :4] = torch.finfo(torch.float32).min                             # all equal: a quarter each
+    val[2, :4] = torch.finfo(torch.float32).max
+    val[3, :4] = 1e7 + torch.tensor([0.0, 1.0, 2.0, 3.0])                    # every value and difference exact
+    val[4, :4] = -1e7 + torch.tensor([3.0, 1.0, 0.0, 2.0])
+    val[5, :4] = torch.tensor([-float("inf"), -3e38, -3e38, -float("inf")])
+    loss, _, d = ctx.distill_loss([logits], [idx], [val], tau)
+    ctx.synchronize()
+    v = val[:, :4].double()
+    p = torch.softmax((v - v.amax(1, keepdim=True)) / tau, 1)
+    logq = torch.log_softmax(logits.double() / tau, 1)
+    q = logq.exp()
+    # p: a quotient of at most 5 off by half a step of 8, an exponential and its sum a few steps; q: a product of at most 12 off by three
+    # half steps of 16, an exponential and a sum of V terms in chains of V / 1024 and joined in twelve steps
+    ep, eq = 32 * F, F * (64 + V / 256)
+    dense = torch.zeros_like(q).scatter_add_(1, idx[:, :4].long(), p)
+    want = tau * (q - dense)
+    close(d[0], want, F * want.abs() + tau * (q * eq + dense * ep) + tiny(torch.float32), "dlogits")
+    terms = torch.where(p > 0, p * (p.clamp(min=1e-300).log() - logq.gather(1, idx[:, :4].long())), torch.zeros_like(p))
+    close(loss[0], tau * tau * terms.sum(1), tau * tau * (terms.abs().sum(1) * ep + eq + ep + 32 * F), "loss")
+
+
 def test_distill_nan_goes_through(ctx):
     mk = Maker(14)
     for V in (300, 140000):
