@@ -443,7 +443,8 @@ uint64_t slimdp_linear_workspace_bytes(uint32_t n_workers, const uint64_t* rows,
  *   logits [rows, vocab]; index, value [rows, top], ldt elements apart, in any order; an index of 0xFFFFFFFF is no entry (lists shorter than
  *   top); an index outside the vocabulary is taken as none and reported by slimdp_synchronize; one that appears twice counts twice.
  *   A row without entries, or of weight 0, has loss 0 and gradient 0, whatever its logits hold.  An entry of value -inf has p = 0 and
- *   adds nothing; a logit of -inf has q = 0, and an infinite loss where p > 0.  NaN values go through.
+ *   adds nothing; a logit of -inf has q = 0, and an infinite loss where p > 0; one of +inf makes lse +inf, the gradient NaN in its own
+ *   place, -w tau p in the others, and the loss infinite, or NaN where p > 0 at such a logit.  NaN values go through.
  *   loss, lse: NULL or [host table] of [dev, rows]; dlogits: NULL or [rows, vocab] (dlogits may be logits).
  *   vocab <= SLIMDP_MAX_VOCAB, top <= SLIMDP_MAX_TEACHER (0: no row has entries, index and value may be NULL); temperature positive and finite. */
 int slimdp_distill_loss(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* rows, uint64_t vocab, uint32_t dtype,

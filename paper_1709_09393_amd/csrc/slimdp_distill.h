@@ -25,6 +25,7 @@ struct DistillArgs {
 // once and written once; the sum's exponentials are taken as the vectors arrive (against each thread's own largest value so far),
 // the gradient's as they leave, and neither waits for the other's memory.  HELD = 0: rows that no block holds, read twice, and calls that ask for no
 // gradient (nothing is kept then: 128,000 columns of bf16, 4,096 rows: 192 us instead of 294).  NT: streams pass the caches by.
+// The largest logit is held finite: one of +inf has an infinite exponential then, no NaN, and lse is infinite.
 // Exponentials are powers of two of (x - largest) * (log2 e / tau): the difference first, so that logits far from zero (a mask of the
 // type's lowest value over a whole row among them) lose nothing to the product's rounding, and the teacher's likewise: a value whose quotient
 // by a temperature below 1 is beyond the type's range is still a value.
@@ -49,7 +50,7 @@ __global__ __launch_bounds__(BT) void k_distill(DistillArgs a)
     const float* row_weight = static_cast<const float*>(a.row_weight.p[q]);
     T* dlogits = static_cast<T*>(a.dlogits.p[q]);
     const float inv_tau = 1.0f / a.tau, scale2 = inv_tau * LOG2E;
-    const float INF = __builtin_inff();
+    const float INF = __builtin_inff(), MOST = __FLT_MAX__;
     // whole vectors, and behind the last of them one element a thread
     const uint32_t main = vocab / V * V, last = main + t;
     const bool has_last = last < vocab;
@@ -135,6 +136,7 @@ __global__ __launch_bounds__(BT) void k_distill(DistillArgs a)
             unpack<T>(v, f);
 #pragma unroll
             for (int i = 0; i < V; ++i) big = fmaxf(big, f[i]);
+            big = fminf(big, MOST);
             if (big > m) {
                 sum *= __builtin_amdgcn_exp2f((m - big) * scale2);             // the first time: 0 * 0
                 m = big;
@@ -144,7 +146,7 @@ __global__ __launch_bounds__(BT) void k_distill(DistillArgs a)
             for (int i = 0; i < V; ++i) sum += __builtin_amdgcn_exp2f((f[i] - ref) * scale2);
         };
         if (has_last) {
-            m = fmaxf(x_last, -INF);
+            m = fminf(fmaxf(x_last, -INF), MOST);
             sum = __builtin_amdgcn_exp2f((x_last - (m == -INF ? 0.0f : m)) * scale2);
         }
         if constexpr (HELD > 0) {

@@ -603,6 +603,40 @@ def test_distill_teacher_values_far_from_zero(ctx, V, top):
     close(loss[0], tau * tau * terms.sum(1), tau * tau * (terms.abs().sum(1) * ep + eq + ep + 32 * F), "loss")
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", [7, 301, 9001, 140001])
+def test_distill_logits_of_plus_infinity(ctx, dtype, V):
+    """lse is infinite; q is 0 beside such a logit and undefined at it; a NaN in the row still goes through.  The last element lies behind
+    the whole vectors."""
+    mk, t = Maker(17), TYPES[dtype]
+    logits = mk.normal(6, V, t)
+    idx = torch.tensor([[1, 2]] * 6, dtype=torch.int32, device="cuda")
+    val = torch.tensor([[0.5, 0.25]] * 6, device="cuda")
+    inf, places = float("inf"), [[V // 2], [V - 1], [0, V - 1], [1], [V // 2], []]
+    for r, at in enumerate(places):
+        for i in at:
+            logits[r, i] = inf
+    logits[4, V - 2] = float("nan")
+    if dtype != "f16":
+        logits[2, 3] = torch.finfo(t).max
+    p = torch.softmax(val.double(), 1)[0]
+    loss, lse, d = ctx.distill_loss([logits], [idx], [val])
+    only, lse2, _ = ctx.distill_loss([logits], [idx], [val], want_grad=False)
+    ctx.synchronize()
+    for e in (lse[0], lse2[0]):
+        assert e[:4].tolist() == [inf] * 4 and bool(e[4].isnan()) and bool(e[5].isfinite())
+    for l in (loss[0], only[0]):
+        assert l[:3].tolist() == [inf] * 3 and bool(l[3:5].isnan().all()) and bool(l[5].isfinite())
+    for r in range(4):
+        own = torch.zeros(V, dtype=torch.bool, device="cuda")
+        own[places[r]] = True
+        want = torch.zeros(V, dtype=torch.float64, device="cuda")
+        want[1], want[2] = -p[0], -p[1]
+        assert bool(d[0][r][own].isnan().all())
+        close(d[0][r][~own], want[~own], 2 * u(t) * want[~own].abs(), f"dlogits {r}")
+    assert bool(d[0][5].isfinite().all())
+
+
 def test_distill_nan_goes_through(ctx):
     mk = Maker(14)
     for V in (300, 140000):
