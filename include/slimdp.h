@@ -380,6 +380,7 @@ enum { SLIMDP_F32 = 0, SLIMDP_F16 = 1, SLIMDP_BF16 = 2 };
 #define SLIMDP_MAX_ROWS (1ull << 24)
 #define SLIMDP_MAX_NORM_COLS 65536ull
 #define SLIMDP_MAX_FEATURES (1ull << 20)
+#define SLIMDP_MAX_TILES (1ull << 23)             /* tiles of 64 x 64 that a product's result may have: 2^35 elements of whole tiles */
 #define SLIMDP_MAX_VOCAB (1ull << 24)
 #define SLIMDP_MAX_TEACHER 1024u
 /* Parameter gradients are added to what the arrays hold instead of replacing it: several calls for one gradient
@@ -409,7 +410,8 @@ uint64_t slimdp_layer_norm_workspace_bytes(uint32_t n_workers, const uint64_t* r
 /* Matrix product with its epilogue:  z = x weight^T + bias,  y = activation(z) + residual.
  *   x [rows, in]; weight [out, in] of the same type; bias: NULL or a table of (NULL or [dev, out]) binary32;
  *   residual: NULL or [rows, out] (y may be residual); y [rows, out]; z: NULL or [rows, out], what the backward pass reads.
- *   y is made from the z before it is rounded.  in, out <= SLIMDP_MAX_FEATURES. */
+ *   y is made from the z before it is rounded.  in, out <= SLIMDP_MAX_FEATURES; ceil(rows / 64) * ceil(out / 64) <= SLIMDP_MAX_TILES (and
+ *   likewise the gradients' [rows, in] and [out, in] below). */
 enum { SLIMDP_ACT_NONE = 0, SLIMDP_ACT_RELU = 1, SLIMDP_ACT_GELU = 2 /* z * normal distribution function of z */,
        SLIMDP_ACT_GELU_TANH = 3 /* 0.5 z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) */, SLIMDP_ACT_SILU = 4 /* z / (1 + exp(-z)) */ };
 int slimdp_linear(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* rows, uint64_t in, uint64_t out, uint32_t dtype,

@@ -34,6 +34,7 @@ GRAD_ACCUMULATE = 1
 MAX_ROWS = 1 << 24
 MAX_NORM_COLS = 65536
 MAX_FEATURES = 1 << 20
+MAX_TILES = 1 << 23
 MAX_VOCAB = 1 << 24
 MAX_TEACHER = 1024
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}

@@ -316,6 +316,14 @@ struct Product {
     uint64_t ws() const { return std::max(bytes(registers(), *this), es == 2 ? bytes(copies(), *this) : 0); }
 };
 
+// What a grid can number, whichever the tile; asked before a call's first launch.
+void tiles_fit(Call& c, const Product& p)
+{
+    if (c.ok() && p.tiles(64) > SLIMDP_MAX_TILES)
+        c.rc = host_fail(c.ctx, SLIMDP_ERR_OUT_OF_RANGE, "%s: a result of %llu x %llu has more than %llu tiles of 64 x 64", c.who,
+                         (unsigned long long)p.M, (unsigned long long)p.N, (unsigned long long)SLIMDP_MAX_TILES);
+}
+
 // How the tile kernel takes sixteen-bit operands: not at all (2: rows shorter than a vector, or distances that do not fit its offsets), through
 // registers (1), or copied into the LDS as they lie (0: whole vectors on their own alignment).
 template <bool AK, bool BK> int staging(const Call& c, const GemmArgs& a, const Product& p)
@@ -333,7 +341,6 @@ template <bool AK, bool BK> int staging(const Call& c, const GemmArgs& a, const 
 template <bool AK, bool BK, int EPI> int product(Call& c, GemmArgs a, const Product& p, uint32_t dtype, void* ws)
 {
     if (p.M == 0 || p.N == 0) return c.rc;
-    if (p.tiles(64) > (1u << 23)) return c.rc = host_fail(c.ctx, SLIMDP_ERR_OUT_OF_RANGE, "%s: more than 2^23 tiles of 64 x 64", c.who);
     a.rows = c.tab;
     a.M = (uint32_t)p.M; a.N = (uint32_t)p.N; a.K = (uint32_t)p.K;
     a.partial = static_cast<float*>(ws);
@@ -576,13 +583,15 @@ int slimdp_linear(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* rows, uin
     c.distinct("y", y, true);
     c.distinct("z", z, true);
     c.workspace(workspace, workspace_bytes, slimdp_linear_workspace_bytes(n_workers, rows, in, out, dtype, SLIMDP_LINEAR_FORWARD));
+    const Product p = forward_product(c.W, c.most, in, out, c.esize);
+    tiles_fit(c, p);
     if (!c.ok()) return c.rc;
     GemmArgs a{};
     a.a = c.in(x); a.b = c.in(weight); a.bias = c.in(bias); a.residual = c.in(residual);
     a.c = c.out(y); a.z = c.out(z);
     a.lda = ldx; a.ldb = ldw; a.ldc = ldy; a.ldr = ldr; a.ldz = ldz;
     a.act = (int)activation;
-    return product<false, false, 0>(c, a, forward_product(c.W, c.most, in, out, c.esize), dtype, workspace);
+    return product<false, false, 0>(c, a, p, dtype, workspace);
 }
 
 int slimdp_linear_epilogue_backward(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* rows, uint64_t out, uint32_t dtype,
@@ -639,6 +648,8 @@ int slimdp_linear_backward(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* 
     if (c.ok() && dweight)
         for (uint32_t q = 0; q < n_workers; ++q)
             if (!dweight[q]) c.rc = host_fail(ctx, SLIMDP_ERR_INVALID_ARG, "slimdp_linear_backward: dweight[%u] is NULL", q);
+    if (dx) tiles_fit(c, pi);
+    if (dweight) tiles_fit(c, pw);
     c.workspace(workspace, workspace_bytes, std::max(dx ? pi.ws() : 0, dweight ? pw.ws() : 0));
     if (!c.ok()) return c.rc;
     if (dx) {

@@ -995,6 +995,25 @@ def test_refusals_of_the_c_entries(ctx):
     ctx.synchronize()
 
 
+def test_results_of_more_tiles_than_a_grid_numbers_are_refused_before_anything_runs(ctx):
+    """Also where the second of a call's two products is the one that is too large: the first is not launched either."""
+    import ctypes as C
+    L, h, most = ctx._L, ctx._h, binding.MAX_FEATURES
+    keep, ws = torch.full((4096,), 5.0, device="cuda"), torch.zeros(1 << 20, device="cuda")
+    o, a = (C.c_void_p * 1)(keep.data_ptr()), (C.c_void_p * 1)(ws.data_ptr())
+    b = (C.c_void_p * 1)(ws.data_ptr() + 4096)
+    n = (C.c_uint64 * 1)(4)
+    assert -(-most // 64) ** 2 > binding.MAX_TILES >= -(-4 // 64) * -(-most // 64)
+    rc = L.slimdp_linear_backward(h, 1, n, most, most, 0, a, most, b, most, b, most, o, most, (C.c_void_p * 1)(ws.data_ptr() + 8192), 0, ws.data_ptr(), 1 << 62)
+    assert rc == binding.ERR_OUT_OF_RANGE and b"tiles" in L.slimdp_last_error(h)
+    n = (C.c_uint64 * 1)(binding.MAX_ROWS)
+    assert L.slimdp_linear(h, 1, n, 8, 2049, 0, a, 8, b, 8, None, 0, None, 0, o, 2049, None, 0, ws.data_ptr(), 1 << 62) == binding.ERR_OUT_OF_RANGE
+    assert b"tiles" in L.slimdp_last_error(h)
+    assert L.slimdp_linear_backward(h, 1, n, 2049, 8, 0, a, 8, None, 0, b, 2049, o, 2049, None, 0, ws.data_ptr(), 1 << 62) == binding.ERR_OUT_OF_RANGE
+    ctx.synchronize()
+    assert bool((keep == 5.0).all())
+
+
 def check_products(ctx, mk, R, K, N, t, what):
     x, w, dz, res = mk.normal(R, K, t), mk.normal(N, K, t, 0.03), mk.normal(R, N, t, 0.1), mk.normal(R, N, t)
     b, old = mk.vec(N), mk.vec(N * K).view(N, K)
