@@ -24,7 +24,19 @@ struct GemmArgs {
     uint32_t splits, k_split;    // the sum in pieces of k_split (a multiple of the step), one block each
     float* partial;              // [worker][split][M][N] where splits > 1
     int act, accumulate;
+    uint32_t first[MAXW_T + 1];  // blocks of the workers before each, and of all (kernels that number only the blocks that have work)
 };
+
+// The worker that a block belongs to: the last one whose blocks begin at or before it.
+__device__ __forceinline__ uint32_t worker_of(const uint32_t (&first)[MAXW_T + 1], uint32_t unit)
+{
+    static_assert(MAXW_T == 32, "five halvings");
+    uint32_t q = 0;
+#pragma unroll
+    for (uint32_t half = 16; half; half >>= 1)
+        if (unit >= first[q + half]) q += half;
+    return q;
+}
 
 // 16 bytes of either operand a lane: eight products' steps of sixteen-bit elements in one instruction, four of binary32 in one each.
 template <class T> struct Mma;
@@ -142,17 +154,15 @@ __device__ __forceinline__ void epilogue4(const GemmArgs& a, uint32_t q, uint32_
     }
 }
 
-// S x S of C a block of four waves (a quarter each, in 16 x 16 accumulators), 128 bytes of k a step.  The next step's
-// pieces are loaded into registers while this one's are multiplied from shared memory; there either operand lies with k running,
-// 128 bytes a row, its eight vectors exchanged by the row's number so that the sixteen rows that a read touches meet
-// different banks.  Operands with rows of k are turned over in registers on the way.  Any size, stride and alignment: what lies
-// outside reads as zero.  S = 64 where 128 would leave compute units without a block; such blocks wait for their loads, and have two
-// steps' under way.  NARROW: rows shorter than a vector, element by element.
+// Rows shorter than a vector, and sixteen-bit operands whose distances do not fit the tile kernel's offsets: 64 x 64 of C a block of four
+// waves, 128 bytes of k a step, element by element where a row breaks off.  In the LDS either operand lies with k running, 128 bytes a row,
+// its eight vectors exchanged by the row's number so that the sixteen rows that a read touches meet different banks; operands with
+// rows of k are turned over in registers on the way.  What lies outside reads as zero.
 // grid (tiles, 1, workers * splits)
-template <class T, bool AK, bool BK_, int EPI, uint32_t S, bool NARROW>
+template <class T, bool AK, bool BK_, int EPI>
 __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
 {
-    constexpr uint32_t V = Vec<T>::N, BK = 8 * V, F = S / 32, RUN = S / 32;
+    constexpr uint32_t V = Vec<T>::N, BK = 8 * V, S = 64, F = S / 32, RUN = S / 32;
     __shared__ raw4 sa[S * 8], sb[S * 8];
     const uint32_t q = blockIdx.z / a.splits, split = blockIdx.z % a.splits;
     const uint32_t M = a.k_is_rows ? a.M : a.rows.n[q], N = a.N, Kall = a.k_is_rows ? a.rows.n[q] : a.K;
@@ -166,55 +176,30 @@ __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
     // one operand's pieces of a step: RUN vectors a thread with k running, one square of V x V elements otherwise
     constexpr uint32_t SQ = S / V * 8;                             // squares of a tile
     constexpr int RA = AK ? (int)V : (int)RUN, RB = BK_ ? (int)V : (int)RUN;
-    constexpr uint32_t DEPTH = S == 64 && !NARROW ? 2 : 1;
-    raw4 ra[DEPTH][RA], rb[DEPTH][RB];
-    // Every load is made, from a place inside the matrix (the last row or vector in place of what lies outside), and what does not belong is
-    // cleared when it is put into the LDS: a load behind a condition of its own waits for the ones before it (2048 x 4096 x 4096 bf16 with
-    // rows of k for either operand 368 us).
+    raw4 ra[RA], rb[RB];
     auto load = [&](auto krows, const T* P, uint64_t ld, uint32_t x0, uint32_t X, uint32_t kb, uint32_t tt, auto& reg) {
         if constexpr (!decltype(krows)::value) {
 #pragma unroll
             for (uint32_t i = 0; i < RUN; ++i) {
                 const uint32_t x = x0 + (t >> 3) + 32u * i, k = kb + (t & 7u) * V;
-                if constexpr (NARROW) reg[i] = x < X && k < K ? load_clip(P + (size_t)x * ld, k, K) : raw4{0, 0, 0, 0};
-                else reg[i] = load_raw<T>(P + (size_t)min(x, X - 1) * ld + min(k, Kall - V));
+                reg[i] = x < X && k < K ? load_clip(P + (size_t)x * ld, k, K) : raw4{0, 0, 0, 0};
             }
         } else {
             if (tt >= SQ) return;
             const uint32_t x = x0 + (tt >> 3) * V, kr = kb + (tt & 7u) * V;        // eight lanes: a whole row of the LDS to write
 #pragma unroll
-            for (uint32_t i = 0; i < V; ++i) {
-                if constexpr (NARROW) reg[i] = x < X && kr + i < K ? load_clip(P + (size_t)(kr + i) * ld, x, X) : raw4{0, 0, 0, 0};
-                else reg[i] = load_raw<T>(P + (size_t)min(kr + i, K - 1) * ld + min(x, X - V));
-            }
+            for (uint32_t i = 0; i < V; ++i) reg[i] = x < X && kr + i < K ? load_clip(P + (size_t)(kr + i) * ld, x, X) : raw4{0, 0, 0, 0};
         }
     };
-    auto put = [&](auto krows, raw4* s, uint32_t x0, uint32_t X, uint32_t kb, uint32_t tt, auto& reg) {
+    auto put = [&](auto krows, raw4* s, uint32_t tt, auto& reg) {
         if constexpr (!decltype(krows)::value) {
-            const uint32_t k = kb + (t & 7u) * V;
 #pragma unroll
             for (uint32_t i = 0; i < RUN; ++i) {
                 const uint32_t x = (t >> 3) + 32u * i;
-                if constexpr (!NARROW) {
-                    if (k < K && k + V > K) reg[i] = move_down<T>(reg[i], k + V - K);
-                    if (k >= K || x0 + x >= X) reg[i] = raw4{0, 0, 0, 0};
-                }
                 s[x * 8 + ((t & 7u) ^ ((x >> 1) & 7u))] = reg[i];
             }
         } else if (tt < SQ) {
-            const uint32_t x = (tt >> 3) * V, ck = tt & 7u, kr = kb + ck * V;
-            if constexpr (!NARROW) {
-                const uint32_t end = x0 + x + V;
-                if (end > X) {
-#pragma unroll
-                    for (uint32_t i = 0; i < V; ++i) reg[i] = end < X + V ? move_down<T>(reg[i], end - X) : raw4{0, 0, 0, 0};
-                }
-                if (kr + V > K) {
-#pragma unroll
-                    for (uint32_t i = 0; i < V; ++i)
-                        if (kr + i >= K) reg[i] = raw4{0, 0, 0, 0};
-                }
-            }
+            const uint32_t x = (tt >> 3) * V, ck = tt & 7u;
             transpose<T>(reg);
 #pragma unroll
             for (uint32_t i = 0; i < V; ++i) s[(x + i) * 8 + (ck ^ (((x + i) >> 1) & 7u))] = reg[i];
@@ -229,16 +214,17 @@ __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
     for (uint32_t i = 0; i < F; ++i)
 #pragma unroll
         for (uint32_t j = 0; j < F; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    auto load_step = [&](uint32_t kb, uint32_t d) {
-        load(ak_t{}, A, a.lda, m0, M, kb, ta, ra[d]);
-        load(bk_t{}, B, a.ldb, n0, N, kb, tb, rb[d]);
+    auto load_step = [&](uint32_t kb) {
+        load(ak_t{}, A, a.lda, m0, M, kb, ta, ra);
+        load(bk_t{}, B, a.ldb, n0, N, kb, tb, rb);
     };
-    auto step = [&](uint32_t kb, uint32_t d) {
+    if (k0 < K) load_step(k0);
+    for (uint32_t kb = k0; kb < K; kb += BK) {
         __syncthreads();
-        put(ak_t{}, sa, m0, M, kb, ta, ra[d]);
-        put(bk_t{}, sb, n0, N, kb, tb, rb[d]);
+        put(ak_t{}, sa, ta, ra);
+        put(bk_t{}, sb, tb, rb);
         __syncthreads();
-        if (kb + DEPTH * BK < K) load_step(kb + DEPTH * BK, d);
+        if (kb + BK < K) load_step(kb + BK);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             raw4 fa[F], fb[F];
@@ -257,15 +243,6 @@ __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
 #pragma unroll
                     for (uint32_t j = 0; j < F; ++j) acc[i][j] = Mma<T>::part(fb[j], fa[i], acc[i][j], e);
         }
-    };
-    if (k0 < K) {
-#pragma unroll
-        for (uint32_t d = 0; d < DEPTH; ++d)
-            if (k0 + d * BK < K) load_step(k0 + d * BK, d);
-        for (uint32_t kb = k0; kb < K; kb += DEPTH * BK)
-#pragma unroll
-            for (uint32_t d = 0; d < DEPTH; ++d)
-                if (kb + d * BK < K) step(kb + d * BK, d);
     }
 #pragma unroll
     for (uint32_t i = 0; i < F; ++i) {
@@ -277,19 +254,18 @@ __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
             if (n >= N) continue;
             const float s[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
             if (a.splits == 1) epilogue4<T, EPI>(a, q, m, n, N, s);
-            else {
-                store4(a.partial + (((size_t)q * a.splits + split) * a.M + m) * N + n, N - n, s);
-            }
+            else store4(a.partial + (((size_t)q * a.splits + split) * a.M + m) * N + n, N - n, s);
         }
     }
 }
 
-// Few rows (up to 16 * MF): the second operand's bytes are all there is to wait for.  It goes from memory to registers as the instructions
+// Few rows (up to 16 * MF) of sixteen-bit types: the second operand's bytes are most of what there is to wait for (every block reads all of the
+// first from the caches, M / 16 times the bytes of its own rows).  It goes from memory to registers as the instructions
 // take it (16 rows, four vectors of each at a time), every element once; a block has 16 of its rows and its eight waves a share of k
 // each, whose sums meet in the LDS in the order of the waves.  A wave has four to eight steps' vectors under way,
 // the number that leaves the fewest places empty in its share (four of 64 rows: more do not fit the registers), and asks for all of them
 // without a condition, from a place inside the row: loads behind a condition each took 57 us instead of 40 at 8 x 50 x 1024 x 4096 bf16,
-// 25.8 instead of 18.6 at 4 x 33 x 1000 x 4000, 58 instead of 45 at 64 x 4096 x 4096 binary32.  4 x 8 x 8192 x 8192 bf16 122 us (4.4 TB/s).
+// 25.8 instead of 18.6 at 4 x 33 x 1000 x 4000.  4 x 8 x 8192 x 8192 bf16 122 us (4.4 TB/s).
 // grid (ceil(N / 16), 1, workers)
 template <class T, int MF, int EPI>
 __global__ __launch_bounds__(512) void k_gemm_few(GemmArgs a)
@@ -382,9 +358,11 @@ __global__ __launch_bounds__(256) void k_gemm_join(GemmArgs a)
     const uint32_t q = blockIdx.z, M = a.k_is_rows ? a.M : a.rows.n[q], N = a.N;
     const uint32_t n = (blockIdx.x * 256 + threadIdx.x) * 4;
     if (n >= N) return;
+    // a worker whose sum is shorter than the longest has fewer pieces (kernels that take all of them write zeros, which add nothing)
+    const uint32_t pieces = a.k_is_rows ? max(1u, (a.rows.n[q] + a.k_split - 1) / a.k_split) : a.splits;
     for (uint32_t m = blockIdx.y; m < M; m += gridDim.y) {
         float s[4] = {0.f, 0.f, 0.f, 0.f};
-        for (uint32_t p = 0; p < a.splits; ++p) {
+        for (uint32_t p = 0; p < pieces; ++p) {
             float x[4];
             load4(a.partial + (((size_t)q * a.splits + p) * a.M + m) * N + n, N - n, x);
 #pragma unroll

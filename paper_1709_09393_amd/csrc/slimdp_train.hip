@@ -12,6 +12,7 @@
 #include "slimdp_norm.h"
 #include "slimdp_linear.h"
 #include "slimdp_gemm.h"
+#include "slimdp_gemm32.h"
 #include "slimdp_distill.h"
 
 using namespace slimdp;
@@ -273,15 +274,15 @@ template <bool NORM> int column_grads(Call& c, ColumnArgs a, uint32_t dtype, int
 struct Product {
     uint64_t M, N, K;
     uint32_t W;
+    const uint64_t* rows;
     size_t es;
     bool rows_of_k;              // K is the number of rows
 
-    struct Cut { uint32_t tile; uint64_t tiles, splits, piece; double us; };
+    struct Cut { uint32_t bm, bn; uint64_t tiles, splits, piece; double us; };
     uint64_t tiles(uint32_t t) const { return ceil_div(M, t) * ceil_div(N, t); }
-    // What a cut takes, as measured: `slots` blocks run at a time over the 256 compute units, `step` us for a step of all of them (less
+    // Sixteen-bit types, as measured: `slots` blocks run at a time over the 256 compute units, `step` us for a step of all of them (less
     // where there is one block to a unit at most), `ends` us to begin and to write, and where the sum is cut the pieces' way to memory and back at
     // 4 TB/s.  Products of 8192 x 8192 x 8192 and 8 x 2048 x 4096 x 4096, bf16: 1.45 us a step with 256 x 256, 0.95 with two of 128 x 128.
-    // Through registers, binary32: 3.6 with two of 128 x 128, 2.0 with four of 64 x 64.
     struct Kernel { uint32_t tile, slots; double step, alone, ends; };
     Cut cut(const Kernel& k, uint64_t want) const
     {
@@ -290,7 +291,7 @@ struct Product {
         const double step = blocks <= 256 ? k.alone : k.step;
         double us = (double)ceil_div(blocks, k.slots) * ((double)per * step + k.ends);
         if (splits > 1) us += 4.0 + (double)(W * splits * M * N) * 8.0 / 4e6;
-        return {k.tile, tiles(k.tile), splits, per * bk, us};
+        return {k.tile, k.tile, tiles(k.tile), splits, per * bk, us};
     }
     Cut best(const Kernel& big, const Kernel& small) const
     {
@@ -304,16 +305,63 @@ struct Product {
     }
     // by copies into the LDS: sixteen-bit types
     Cut copies() const { return best({256, 256, 1.45, 1.45, 12.0}, {128, 512, 0.95, 0.65, 8.0}); }
-    // through registers: binary32; and sixteen-bit types that cannot be copied, and rows shorter than a vector, element by element with 64 x 64
-    bool narrow() const { return es == 2 || std::min(N, rows_of_k ? M : K) < 4; }
-    Cut registers() const
+    // rows shorter than a vector, and what the copies do not reach: element by element
+    Cut elements() const
     {
-        const Kernel small = {64, 1024, 2.0, 0.7, 6.0};
-        return narrow() ? best(small, small) : best({128, 512, 3.6, 2.2, 8.0}, small);
+        const Kernel k = {64, 1024, 2.0, 0.7, 6.0};
+        return best(k, k);
     }
-    bool few() const { return !rows_of_k && M <= 64; }
+    // Binary32.  A block's step is 32 of k.  One block to a compute unit takes `alone` us for it, several share the unit at `step` each;
+    // `begin` us a block of 64 x 64 for what is no step, 18 TB/s for what all blocks read together (the caches' rate), and where the sum
+    // is cut a second launch and the pieces' way to memory and back.  Fitted to the times of 4,100 products of 1 to 16,384 rows, 16 to 8192 in and
+    // out, forward and backward, one to eight workers, with every tile and 1 to 48 pieces: the cut that these constants choose takes 2 %
+    // more than the fastest on average (1.5 times at worst, of calls of 15 to 80 us).
+    struct Tile { uint32_t bm, bn; double step, alone; };
+    // Blocks of one worker.
+    uint64_t blocks32(uint32_t q, uint32_t bm, uint32_t bn, uint64_t splits, uint64_t piece) const
+    {
+        if (rows_of_k) return ceil_div(M, bm) * ceil_div(N, bn) * std::max<uint64_t>(1, ceil_div(rows[q], piece));
+        return ceil_div(rows[q], bm) * ceil_div(N, bn) * splits;
+    }
+    Cut tiles32() const
+    {
+        static const Tile list[] = {{64, 64, 0.42, 0.47}, {32, 64, 0.24, 0.47}, {32, 32, 0.135, 0.16}, {16, 64, 0.18, 0.18}, {64, 16, 0.18, 0.18}};
+        const uint64_t steps = ceil_div(K, 32);
+        double results = 0;
+        for (uint32_t q = 0; q < W; ++q) results += (double)(rows_of_k ? M : rows[q]) * (double)N;
+        Cut b{};
+        for (const Tile& t : list) {
+            // tiles of all workers, and the steps of all tiles where nothing is cut
+            uint64_t tiles = 0, all = 0;
+            for (uint32_t q = 0; q < W; ++q) {
+                const uint64_t n = rows_of_k ? ceil_div(M, t.bm) * ceil_div(N, t.bn) : ceil_div(rows[q], t.bm) * ceil_div(N, t.bn);
+                tiles += n;
+                all += n * (rows_of_k ? std::max<uint64_t>(1, ceil_div(rows[q], 32)) : steps);
+            }
+            const double area = t.bm * t.bn / 4096.0, read = (double)all * (t.bm + t.bn) * 128.0 / 18e6;
+            uint64_t last = 0;
+            for (const uint64_t want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48}) {
+                const uint64_t per = std::max<uint64_t>(1, ceil_div(steps, want)), splits = std::max<uint64_t>(1, ceil_div(steps, per));
+                if (splits == last) continue;
+                last = splits;
+                if (tiles * splits > (1ull << 24) && (splits > 1 || t.bm * t.bn < 4096)) break;
+                const double n = (double)all / (double)per / 256.0, whole = std::ceil(n);
+                double us = std::max({(double)per * t.alone, (whole <= 8 ? whole : n) * ((double)per * t.step + 0.09 * area), read});
+                if (splits > 1) us += 6.0 + results * (double)splits * 8.0 / 2e6;
+                if (!b.bm || us < b.us) b = {t.bm, t.bn, tiles, splits, per * 32, us};
+            }
+        }
+        return b;
+    }
+    // ... of rows that no vector fits in
+    bool narrow() const { return std::min(N, rows_of_k ? M : K) < 4; }
+    bool few() const { return es == 2 && !rows_of_k && M <= 64 && ceil_div(N, 16) * W >= 64; }
     static uint64_t bytes(const Cut& c, const Product& p) { return c.splits > 1 ? p.W * c.splits * p.M * p.N * 4 : 0; }
-    uint64_t ws() const { return std::max(bytes(registers(), *this), es == 2 ? bytes(copies(), *this) : 0); }
+    uint64_t ws() const
+    {
+        if (es == 2) return std::max(bytes(elements(), *this), bytes(copies(), *this));
+        return bytes(narrow() ? elements() : tiles32(), *this);
+    }
 };
 
 // What a grid can number, whichever the tile; asked before a call's first launch.
@@ -338,6 +386,17 @@ template <bool AK, bool BK> int staging(const Call& c, const GemmArgs& a, const 
     return p.es == 2 ? std::max(of(a.a, a.lda, AK ? p.M : p.K), of(a.b, a.ldb, BK ? p.N : p.K)) : 2;
 }
 
+// The second launch of a product whose sum was cut.
+template <class T, int EPI> int joined(Call& c, const GemmArgs& a, const Product& p)
+{
+    if (c.ok() && a.splits > 1)
+        c.launched("k_gemm_join", [&] {
+            hipLaunchKernelGGL((k_gemm_join<T, EPI>), dim3((uint32_t)ceil_div(p.N, 1024), (uint32_t)std::min<uint64_t>(p.M, 1024), c.W),
+                               dim3(256), 0, c.v.stream, a);
+        });
+    return c.rc;
+}
+
 template <bool AK, bool BK, int EPI> int product(Call& c, GemmArgs a, const Product& p, uint32_t dtype, void* ws)
 {
     if (p.M == 0 || p.N == 0) return c.rc;
@@ -345,10 +404,34 @@ template <bool AK, bool BK, int EPI> int product(Call& c, GemmArgs a, const Prod
     a.M = (uint32_t)p.M; a.N = (uint32_t)p.N; a.K = (uint32_t)p.K;
     a.partial = static_cast<float*>(ws);
     a.splits = 1;
+    if (dtype == SLIMDP_F32 && !p.narrow()) {
+        const Product::Cut cut = p.tiles32();
+        a.splits = (uint32_t)cut.splits;
+        a.k_split = (uint32_t)cut.piece;
+        uint64_t blocks = 0;
+        for (uint32_t q = 0; q < MAXW_T; ++q) {
+            a.first[q] = (uint32_t)blocks;
+            if (q < c.W) blocks += p.blocks32(q, cut.bm, cut.bn, cut.splits, cut.piece);
+        }
+        a.first[MAXW_T] = (uint32_t)blocks;
+        constexpr uint64_t ACROSS = 1u << 20;
+        auto launch = [&](auto kernel) {
+            c.launched("k_gemm32", [&] {
+                const dim3 grid((uint32_t)std::min(blocks, ACROSS), (uint32_t)ceil_div(blocks, ACROSS));
+                hipLaunchKernelGGL(kernel, grid, dim3(256), 0, c.v.stream, a);
+            });
+        };
+        if (cut.bm == 64 && cut.bn == 64) launch(k_gemm32<AK, BK, EPI, 64, 64, 2, 2>);
+        else if (cut.bm == 32 && cut.bn == 64) launch(k_gemm32<AK, BK, EPI, 32, 64, 1, 4>);
+        else if (cut.bm == 32) launch(k_gemm32<AK, BK, EPI, 32, 32, 2, 2>);
+        else if (cut.bm == 16) launch(k_gemm32<AK, BK, EPI, 16, 64, 1, 4>);
+        else launch(k_gemm32<AK, BK, EPI, 64, 16, 4, 1>);
+        return joined<float, EPI>(c, a, p);
+    }
     if constexpr (!AK && !BK) {
         // few rows against many: 16 rows of weights a block
-        if (p.few() && ceil_div(p.N, 16) * c.W >= 64) {
-            with_type(dtype, [&](auto z) {
+        if (p.few()) {
+            auto of = [&](auto z) {
                 typedef decltype(z) T;
                 auto launch = [&](auto kernel) {
                     c.launched("k_gemm_few", [&] {
@@ -358,12 +441,13 @@ template <bool AK, bool BK, int EPI> int product(Call& c, GemmArgs a, const Prod
                 if (p.M <= 16) launch(k_gemm_few<T, 1, EPI>);
                 else if (p.M <= 32) launch(k_gemm_few<T, 2, EPI>);
                 else launch(k_gemm_few<T, 4, EPI>);
-            });
+            };
+            if (dtype == SLIMDP_F16) of(_Float16{}); else of(__bf16{});
             return c.rc;
         }
     }
     const int stage = staging<AK, BK>(c, a, p);
-    const Product::Cut cut = stage < 2 ? p.copies() : p.registers();
+    const Product::Cut cut = stage < 2 ? p.copies() : p.elements();
     a.splits = (uint32_t)cut.splits;
     a.k_split = (uint32_t)cut.piece;
     const dim3 grid((uint32_t)cut.tiles, 1, c.W * a.splits);
@@ -373,33 +457,30 @@ template <bool AK, bool BK, int EPI> int product(Call& c, GemmArgs a, const Prod
             auto launch = [&](auto kernel) {
                 c.launched("k_gemm_tiles", [&] { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, c.v.stream, a); });
             };
-            if (stage == 0 && cut.tile == 256) launch(k_gemm_tiles<T, AK, BK, EPI, 256, 256, 2, 2, 1, true>);
+            if (stage == 0 && cut.bm == 256) launch(k_gemm_tiles<T, AK, BK, EPI, 256, 256, 2, 2, 1, true>);
             else if (stage == 0) launch(k_gemm_tiles<T, AK, BK, EPI, 128, 128, 2, 2, 2, true>);
-            else if (stage == 1 && cut.tile == 256) launch(k_gemm_tiles<T, AK, BK, EPI, 256, 256, 2, 2, 1, false>);
+            else if (stage == 1 && cut.bm == 256) launch(k_gemm_tiles<T, AK, BK, EPI, 256, 256, 2, 2, 1, false>);
             else if (stage == 1) launch(k_gemm_tiles<T, AK, BK, EPI, 128, 128, 2, 2, 2, false>);
         }
-        if (stage == 2) {
-            auto launch = [&](auto kernel) {
-                c.launched("k_gemm", [&] { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, c.v.stream, a); });
-            };
-            if (p.narrow()) launch(k_gemm<T, AK, BK, EPI, 64, true>);
-            else if constexpr (sizeof(T) == 4) {
-                if (cut.tile == 128) launch(k_gemm<T, AK, BK, EPI, 128, false>);
-                else launch(k_gemm<T, AK, BK, EPI, 64, false>);
-            }
-        }
-        if (c.ok() && a.splits > 1)
-            c.launched("k_gemm_join", [&] {
-                hipLaunchKernelGGL((k_gemm_join<T, EPI>), dim3((uint32_t)ceil_div(p.N, 1024), (uint32_t)std::min<uint64_t>(p.M, 1024), c.W),
-                                   dim3(256), 0, c.v.stream, a);
-            });
+        if (stage == 2)
+            c.launched("k_gemm", [&] { hipLaunchKernelGGL((k_gemm<T, AK, BK, EPI>), grid, dim3(256), 0, c.v.stream, a); });
+        joined<T, EPI>(c, a, p);
     });
     return c.rc;
 }
 
-Product forward_product(uint32_t W, uint64_t most, uint64_t in, uint64_t out, size_t es) { return {most, out, in, W, es, false}; }
-Product input_product(uint32_t W, uint64_t most, uint64_t in, uint64_t out, size_t es) { return {most, in, out, W, es, false}; }
-Product weight_product(uint32_t W, uint64_t most, uint64_t in, uint64_t out, size_t es) { return {out, in, most, W, es, true}; }
+Product forward_product(uint32_t W, const uint64_t* rows, uint64_t in, uint64_t out, size_t es)
+{
+    return {most_rows(W, rows), out, in, W, rows, es, false};
+}
+Product input_product(uint32_t W, const uint64_t* rows, uint64_t in, uint64_t out, size_t es)
+{
+    return {most_rows(W, rows), in, out, W, rows, es, false};
+}
+Product weight_product(uint32_t W, const uint64_t* rows, uint64_t in, uint64_t out, size_t es)
+{
+    return {out, in, most_rows(W, rows), W, rows, es, true};
+}
 
 }  // namespace
 
@@ -552,9 +633,9 @@ uint64_t slimdp_linear_workspace_bytes(uint32_t n_workers, const uint64_t* rows,
         return 0;
     const size_t es = dtype == SLIMDP_F32 ? 4 : 2;
     const uint64_t most = most_rows(n_workers, rows);
-    if (pass == SLIMDP_LINEAR_FORWARD) return forward_product(n_workers, most, in, out, es).ws();
+    if (pass == SLIMDP_LINEAR_FORWARD) return forward_product(n_workers, rows, in, out, es).ws();
     if (pass == SLIMDP_LINEAR_EPILOGUE_BACKWARD) return column_ws(most, n_workers, out, es, 1);
-    return std::max(input_product(n_workers, most, in, out, es).ws(), weight_product(n_workers, most, in, out, es).ws());
+    return std::max(input_product(n_workers, rows, in, out, es).ws(), weight_product(n_workers, rows, in, out, es).ws());
 }
 
 int slimdp_linear(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* rows, uint64_t in, uint64_t out, uint32_t dtype,
@@ -583,7 +664,7 @@ int slimdp_linear(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* rows, uin
     c.distinct("y", y, true);
     c.distinct("z", z, true);
     c.workspace(workspace, workspace_bytes, slimdp_linear_workspace_bytes(n_workers, rows, in, out, dtype, SLIMDP_LINEAR_FORWARD));
-    const Product p = forward_product(c.W, c.most, in, out, c.esize);
+    const Product p = forward_product(c.W, rows, in, out, c.esize);
     tiles_fit(c, p);
     if (!c.ok()) return c.rc;
     GemmArgs a{};
@@ -644,7 +725,7 @@ int slimdp_linear_backward(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* 
     c.apart("dx", dx, "weight", weight);
     c.distinct("dx", dx, true);
     c.distinct("dweight", dweight, false);
-    const Product pi = input_product(n_workers, c.most, in, out, c.esize), pw = weight_product(n_workers, c.most, in, out, c.esize);
+    const Product pi = input_product(n_workers, rows, in, out, c.esize), pw = weight_product(n_workers, rows, in, out, c.esize);
     if (c.ok() && dweight)
         for (uint32_t q = 0; q < n_workers; ++q)
             if (!dweight[q]) c.rc = host_fail(ctx, SLIMDP_ERR_INVALID_ARG, "slimdp_linear_backward: dweight[%u] is NULL", q);

@@ -1055,3 +1055,78 @@ def test_few_rows_with_every_share_of_a_wave(ctx, dtype, R):
     """Rows shorter than a vector, waves without a share, with one to several turns of steps, and ends inside a vector."""
     for pad, shift, K in ((0, 0, 3), (1, 1, 9), (0, 0, 33), (3, 1, 130), (0, 0, 999), (8, 8, 1280), (5, 3, 1290), (0, 0, 2049), (0, 0, 2600), (1, 0, 4111)):
         check_products(ctx, Maker(33, pad, shift), R, K, 1040, TYPES[dtype], f"{dtype} {R} {K}")
+
+
+def check_workers(ctx, rows, K, N, t, pad=0, shift=0):
+    """The three products of several workers, element by element; gradients added up as well."""
+    mk = Maker(34, pad, shift)
+    W, what = len(rows), f"{rows} x {K} x {N} "
+    x, dz, w = [mk.normal(r, K, t) for r in rows], [mk.normal(r, N, t, 0.1) for r in rows], [mk.normal(N, K, t, 0.03) for _ in rows]
+    y, dx, old = [mk.view(r, N, t) for r in rows], [mk.view(r, K, t) for r in rows], [mk.vec(N * K).view(N, K) for _ in rows]
+    add = [v.clone() for v in old]
+    ctx.linear(x, w, y=y)
+    _, dw = ctx.linear_backward(dz, x, w, dx=dx)
+    ctx.linear_backward(dz, x, None, dweight=add, want_dx=False, accumulate=True)
+    ctx.synchronize()
+    for q in range(W):
+        xd, wd, zd = x[q].double(), w[q].double(), dz[q].double()
+        ref = xd @ wd.t()
+        close(y[q], ref, u(t) * ref.abs() + 1.01 * steps(K, t) * F * (xd.abs() @ wd.abs().t()) + tiny(t), what + f"y {q}")
+        ref = zd @ wd
+        close(dx[q], ref, u(t) * ref.abs() + 1.01 * steps(N, t) * F * (zd.abs() @ wd.abs()) + tiny(t), what + f"dx {q}")
+        zt = zd.t().contiguous()
+        ref, e = zt @ xd, 1.01 * steps(rows[q], t) * F * (zt.abs() @ xd.abs()) + 1e-30
+        close(dw[q], ref, F * ref.abs() + e, what + f"dweight {q}")
+        both = ref + old[q].double()
+        close(add[q], both, 1.01 * e + F * (ref.abs() + both.abs()), what + f"dweight added {q}")
+    mk.check_gaps()
+
+
+@pytest.mark.parametrize("rows,K,N", [([1529], 832, 1119), ([24], 3592, 1608), ([58, 3], 1592, 608), ([2500], 1000, 16), ([1300], 24, 700), ([1100], 700, 40),
+                                      ([2300, 0, 1, 33], 130, 97), ([0, 0, 5, 0, 900], 33, 260), ([700, 31, 32, 33, 0, 1, 64, 65], 100, 72), ([5], 4, 4),
+                                      ([31] * 32, 36, 68), ([4000, 20], 17, 19), ([333], 4097, 5), ([9], 5, 4097)])
+def test_products_in_binary32_of_uneven_workers_and_thin_results(ctx, rows, K, N):
+    """Sums in one and in many pieces (fewer of them for workers with few rows), tiles of every width, and edges inside a vector."""
+    for pad, shift in ((0, 0), (3, 1)):
+        check_workers(ctx, rows, K, N, torch.float32, pad, shift)
+
+
+def test_products_in_binary32_of_more_blocks_than_one_dimension_numbers(ctx):
+    rows, K, N = 1 << 20, 4, 4160
+    x, w = torch.randn(rows, K, device="cuda"), torch.randn(N, K, device="cuda")
+    y = torch.full((rows, N), float("nan"), device="cuda")
+    assert -(-rows // 64) * -(-N // 64) > 1 << 20
+    ctx.linear([x], [w], y=[y])
+    ctx.synchronize()
+    wt, mag = w.double().t().contiguous(), w.double().abs().t().contiguous()
+    for a in range(0, rows, 1 << 16):
+        xd = x[a:a + (1 << 16)].double()
+        close(y[a:a + (1 << 16)], xd @ wt, 5 * F * (xd.abs() @ mag), f"rows {a}")           # four products in one instruction's chain
+    del y
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("R,K,N,what", [(58, 3592, 4608, "forward"), (13286, 6638, 16, "forward"), (2048, 2048, 2048, "forward"), (1772, 4388, 264, "dx"),
+                                        (8608, 2496, 16, "dweight"), (1, 960, 6776, "dx")])
+def test_products_in_binary32_keep_up_with_the_elementary_form(R, K, N, what):
+    """Not slower than half again what torch's product takes (58 x 3592 x 4608 and 13,286 x 6638 x 16 once took two and three times it)."""
+    import time
+    sd = binding.SlimDP(100, 1)
+    x, w, dz = (torch.randn(a, b, device="cuda") for a, b in ((R, K), (N, K), (R, N)))
+    y, dx, dw = torch.empty_like(dz), torch.empty_like(x), torch.empty_like(w)
+    own = {"forward": lambda: sd.linear([x], [w], y=[y]), "dx": lambda: sd.linear_backward([dz], None, [w], dx=[dx], want_dweight=False),
+           "dweight": lambda: sd.linear_backward([dz], [x], None, dweight=[dw], want_dx=False)}[what]
+    plain = {"forward": lambda: x @ w.t(), "dx": lambda: dz @ w, "dweight": lambda: dz.t() @ x}[what]
+    torch.cuda.synchronize()
+
+    def once(f):
+        t = time.perf_counter()
+        for _ in range(20):
+            f()
+        torch.cuda.synchronize()
+        return time.perf_counter() - t
+    once(own), once(plain)
+    pairs = [(once(own), once(plain)) for _ in range(9)]
+    a, b = (sorted(p[i] for p in pairs)[4] for i in (0, 1))
+    assert a < 1.5 * b + 20 * 5e-6, (a / 20 * 1e6, b / 20 * 1e6)                            # 5 us: a second launch from the host
+    sd.close()
