@@ -237,7 +237,8 @@ __device__ __forceinline__ void epilogue8(const GemmArgs& a, char* c, const T* r
 // Reads and copies are put between the products one by one: the compiler by itself puts the products first and then waits for the reads.
 // Sums leave through the LDS, WM parts one after the other, so that memory sees whole rows.
 // BLOCKS share a compute unit: one of 256 x 256, or two of 128 x 128.
-// grid (tiles, 1, workers * splits); which tile a block takes goes by the die it runs on (see below).
+// grid: a.blocks, over two dimensions where one does not number them; which tile a block takes goes by the die it runs
+// on (see below).
 template <class T, bool AK, bool BK_, int EPI, uint32_t BM, uint32_t BN, uint32_t WM, uint32_t WN, uint32_t BLOCKS, bool DIRECT>
 __global__ __launch_bounds__(WM * WN * 64, BLOCKS) void k_gemm_tiles(GemmArgs a)
 {
@@ -249,17 +250,23 @@ __global__ __launch_bounds__(WM * WN * 64, BLOCKS) void k_gemm_tiles(GemmArgs a)
     __shared__ __attribute__((aligned(1024))) char lds[LDS];
 
     // Blocks go round the eight dies in turn: a die gets consecutive tiles (of consecutive workers), and takes them eight rows of
-    // tiles at a time, so that what its blocks read at one time lies in few rows and columns.
-    const uint32_t total = gridDim.x * gridDim.z, id = blockIdx.z * gridDim.x + blockIdx.x;
-    const uint32_t die = id & 7u, per = total >> 3, extra = total & 7u;
-    const uint32_t tile = die * per + min(die, extra) + (id >> 3);
-    const uint32_t zz = tile / gridDim.x, tt = tile % gridDim.x;
-    const uint32_t q = zz / a.splits, split = zz % a.splits;
+    // tiles at a time, so that what its blocks read at one time lies in few rows and columns.  Where a tile of one worker takes longer than
+    // another's (a.spread) every die gets its share of every worker instead.  Only tiles that exist are numbered: a worker without rows
+    // leaves no die idle (16,384 x 4096 x 4096 bf16, one worker of eight has all the rows: 450 us; 2,770 where every worker had the tiles of the largest).
+    const uint32_t id = blockIdx.y * gridDim.x + blockIdx.x;
+    if (id >= a.blocks) return;
+    auto dealt = [](uint32_t n, uint32_t count) {
+        const uint32_t die = n & 7u;
+        return die * (count >> 3) + min(die, count & 7u) + (n >> 3);
+    };
+    const uint32_t unit = a.spread ? id : dealt(id, a.blocks);
+    const Share of = share_of(a, unit);
+    const uint32_t q = of.q, local = a.spread ? dealt(unit - of.begin, of.count) : unit - of.begin;
     const uint32_t M = a.k_is_rows ? a.M : a.rows.n[q], N = a.N, Kall = a.k_is_rows ? a.rows.n[q] : a.K;
-    const uint32_t across = (N + BN - 1) / BN, down = gridDim.x / across;
+    const uint32_t across = (N + BN - 1) / BN, down = (M + BM - 1) / BM, tiles = across * down;
+    const uint32_t split = local / tiles, tt = local % tiles;
     const uint32_t group = tt / (8 * across), in_group = tt % (8 * across), high = min(8u, down - group * 8);
     const uint32_t m0 = (group * 8 + in_group % high) * BM, n0 = in_group / high * BN;
-    if (m0 >= M) return;
     const uint32_t k0 = min(Kall, split * a.k_split), K = min(Kall, k0 + a.k_split);
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
 

@@ -84,7 +84,7 @@ template <bool KROWS, uint32_t X> struct Tile32 {
 // 25 us (24).  Tiles are no larger than 64 x 64 because more blocks leave less of the last round empty (1529 x 832 x 3119: 92 us
 // with 128 x 64, 78 so), and narrower where the result is: 13,286 x 6638 x 16 80 us with 64 x 16, 155 with 64 x 64; 24 x 3592 x 4608 22 us
 // with 32 x 64.  Few rows are bound by memory, and so is what has few of k.
-// grid: as many blocks as a.first counts, over two dimensions where one does not number them
+// grid: a.blocks, over two dimensions where one does not number them
 template <bool AK, bool BK_, int EPI, uint32_t BM, uint32_t BN, uint32_t WM, uint32_t WN>
 __global__ __launch_bounds__(256, 4) void k_gemm32(GemmArgs a)
 {
@@ -95,14 +95,15 @@ __global__ __launch_bounds__(256, 4) void k_gemm32(GemmArgs a)
     __shared__ __attribute__((aligned(1024))) char lds[2 * (TA::BYTES + TB::BYTES)];
 
     const uint32_t unit = blockIdx.y * gridDim.x + blockIdx.x;
-    if (unit >= a.first[MAXW_T]) return;
-    const uint32_t q = worker_of(a.first, unit);
+    if (unit >= a.blocks) return;
+    const Share of = share_of(a, unit);
+    const uint32_t q = of.q;
     const uint32_t M = a.k_is_rows ? a.M : a.rows.n[q], N = a.N, Kall = a.k_is_rows ? a.rows.n[q] : a.K;
     const uint32_t across = (N + BN - 1) / BN, down = (M + BM - 1) / BM, tiles = across * down;
     // Blocks go round the eight dies in turn: of every worker a die gets consecutive tiles (workers may differ in what a tile takes), and
     // takes them eight rows of tiles at a time, so that what its blocks read at one time lies in few rows and columns.
-    const uint32_t mine = unit - a.first[q], count = a.first[q + 1] - a.first[q], die = mine & 7u;
-    const uint32_t place_in = die * (count >> 3) + min(die, count & 7u) + (mine >> 3);
+    const uint32_t mine = unit - of.begin, die = mine & 7u;
+    const uint32_t place_in = die * (of.count >> 3) + min(die, of.count & 7u) + (mine >> 3);
     const uint32_t split = place_in / tiles, tt = place_in % tiles;
     const uint32_t group = tt / (8 * across), in_group = tt % (8 * across), high = min(8u, down - group * 8);
     const uint32_t m0 = (group * 8 + in_group % high) * BM, n0 = in_group / high * BN;

@@ -24,18 +24,27 @@ struct GemmArgs {
     uint32_t splits, k_split;    // the sum in pieces of k_split (a multiple of the step), one block each
     float* partial;              // [worker][split][M][N] where splits > 1
     int act, accumulate;
-    uint32_t first[MAXW_T + 1];  // blocks of the workers before each, and of all (kernels that number only the blocks that have work)
+    uint32_t blocks;             // of all workers (kernels that number only the blocks that have work)
+    uint32_t each;               // of every worker, where all have the same number; otherwise 0, and ...
+    uint32_t first[MAXW_T + 1];  // ... of the workers before each, and of all
+    int spread;                  // workers differ in what a block of theirs takes
 };
 
-// The worker that a block belongs to: the last one whose blocks begin at or before it.
-__device__ __forceinline__ uint32_t worker_of(const uint32_t (&first)[MAXW_T + 1], uint32_t unit)
+// The worker that a block belongs to, its first block and the number of its blocks.  (Halving takes five loads one after the other, half a
+// microsecond of a launch: only where the workers differ.)
+struct Share { uint32_t q, begin, count; };
+__device__ __forceinline__ Share share_of(const GemmArgs& a, uint32_t unit)
 {
+    if (a.each) {
+        const uint32_t q = unit / a.each;
+        return {q, q * a.each, a.each};
+    }
     static_assert(MAXW_T == 32, "five halvings");
     uint32_t q = 0;
 #pragma unroll
     for (uint32_t half = 16; half; half >>= 1)
-        if (unit >= first[q + half]) q += half;
-    return q;
+        if (unit >= a.first[q + half]) q += half;
+    return {q, a.first[q], a.first[q + 1] - a.first[q]};
 }
 
 // 16 bytes of either operand a lane: eight products' steps of sixteen-bit elements in one instruction, four of binary32 in one each.
@@ -358,7 +367,7 @@ __global__ __launch_bounds__(256) void k_gemm_join(GemmArgs a)
     const uint32_t q = blockIdx.z, M = a.k_is_rows ? a.M : a.rows.n[q], N = a.N;
     const uint32_t n = (blockIdx.x * 256 + threadIdx.x) * 4;
     if (n >= N) return;
-    // a worker whose sum is shorter than the longest has fewer pieces (kernels that take all of them write zeros, which add nothing)
+    // a worker whose sum is shorter than the longest has fewer pieces
     const uint32_t pieces = a.k_is_rows ? max(1u, (a.rows.n[q] + a.k_split - 1) / a.k_split) : a.splits;
     for (uint32_t m = blockIdx.y; m < M; m += gridDim.y) {
         float s[4] = {0.f, 0.f, 0.f, 0.f};

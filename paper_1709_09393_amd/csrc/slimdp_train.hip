@@ -276,40 +276,61 @@ struct Product {
     uint32_t W;
     const uint64_t* rows;
     size_t es;
-    bool rows_of_k;              // K is the number of rows
+    bool forward, rows_of_k;     // both operands with k running;  K is the number of rows
+    double results = 0;          // elements of all results
+    bool uneven = false;         // sums of different lengths
 
+    // Small calls wait for the host: what the cuts share is found once, and so is a cut.
+    Product(uint64_t m, uint64_t n, uint64_t k, uint32_t w, const uint64_t* r, size_t e, int which)
+        : M(m), N(n), K(k), W(w), rows(r), es(e), forward(which == 0), rows_of_k(which == 2)
+    {
+        for (uint32_t q = 0; q < W; ++q) {
+            results += (double)(rows_of_k ? M : rows[q]) * (double)N;
+            uneven |= rows_of_k && rows[q] != rows[0];
+        }
+    }
     struct Cut { uint32_t bm, bn; uint64_t tiles, splits, piece; double us; };
     uint64_t tiles(uint32_t t) const { return ceil_div(M, t) * ceil_div(N, t); }
     // Sixteen-bit types, as measured: `slots` blocks run at a time over the 256 compute units, `step` us for a step of all of them (less
     // where there is one block to a unit at most), `ends` us to begin and to write, and where the sum is cut the pieces' way to memory and back at
     // 4 TB/s.  Products of 8192 x 8192 x 8192 and 8 x 2048 x 4096 x 4096, bf16: 1.45 us a step with 256 x 256, 0.95 with two of 128 x 128.
     struct Kernel { uint32_t tile, slots; double step, alone, ends; };
-    Cut cut(const Kernel& k, uint64_t want) const
+    Cut cut(const Kernel& k, uint64_t want, uint64_t all) const
     {
         const uint64_t bk = 128 / es, steps = ceil_div(K, bk), per = std::max<uint64_t>(1, ceil_div(steps, want));
-        const uint64_t splits = std::max<uint64_t>(1, ceil_div(steps, per)), blocks = tiles(k.tile) * W * splits;
+        const uint64_t splits = std::max<uint64_t>(1, ceil_div(steps, per)), blocks = ceil_div(all, per);
         const double step = blocks <= 256 ? k.alone : k.step;
-        double us = (double)ceil_div(blocks, k.slots) * ((double)per * step + k.ends);
-        if (splits > 1) us += 4.0 + (double)(W * splits * M * N) * 8.0 / 4e6;
+        // blocks of workers with shorter sums fill the last round up: what all of them take counts, not whole rounds of the longest
+        const double rounds = uneven ? std::max(1.0, (double)all / (double)per / k.slots) : (double)ceil_div(blocks, k.slots);
+        double us = rounds * ((double)per * step + k.ends);
+        if (splits > 1) us += 4.0 + results * (double)splits * 8.0 / 4e6;
         return {k.tile, k.tile, tiles(k.tile), splits, per * bk, us};
+    }
+    // Steps of all the workers' tiles, those without a step counted as one.
+    uint64_t steps_of_all(uint32_t bm, uint32_t bn, uint64_t bk) const
+    {
+        uint64_t n = 0;
+        for (uint32_t q = 0; q < W; ++q) n += rows_of_k ? std::max<uint64_t>(1, ceil_div(rows[q], bk)) : ceil_div(rows[q], bm);
+        return n * ceil_div(N, bn) * (rows_of_k ? ceil_div(M, bm) : ceil_div(K, bk));
     }
     Cut best(const Kernel& big, const Kernel& small) const
     {
-        Cut b = cut(big, 1);
-        for (const uint64_t want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64})
-            for (const Kernel* k : {&big, &small}) {
-                const Cut c = cut(*k, want);
-                if (c.us < b.us) b = c;
-            }
+        const uint64_t all_big = steps_of_all(big.tile, big.tile, 128 / es), all_small = steps_of_all(small.tile, small.tile, 128 / es);
+        Cut b = cut(big, 1, all_big);
+        for (const uint64_t want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+            const Cut c = cut(big, want, all_big), d = cut(small, want, all_small);
+            if (c.us < b.us) b = c;
+            if (d.us < b.us) b = d;
+        }
         return b;
     }
     // by copies into the LDS: sixteen-bit types
-    Cut copies() const { return best({256, 256, 1.45, 1.45, 12.0}, {128, 512, 0.95, 0.65, 8.0}); }
+    const Cut& copies() const { return once(copies_, [&] { return best({256, 256, 1.45, 1.45, 12.0}, {128, 512, 0.95, 0.65, 8.0}); }); }
     // rows shorter than a vector, and what the copies do not reach: element by element
-    Cut elements() const
+    const Cut& elements() const
     {
         const Kernel k = {64, 1024, 2.0, 0.7, 6.0};
-        return best(k, k);
+        return once(elements_, [&] { return best(k, k); });
     }
     // Binary32.  A block's step is 32 of k.  One block to a compute unit takes `alone` us for it, several share the unit at `step` each;
     // `begin` us a block of 64 x 64 for what is no step, 18 TB/s for what all blocks read together (the caches' rate), and where the sum
@@ -317,27 +338,14 @@ struct Product {
     // out, forward and backward, one to eight workers, with every tile and 1 to 48 pieces: the cut that these constants choose takes 2 %
     // more than the fastest on average (1.5 times at worst, of calls of 15 to 80 us).
     struct Tile { uint32_t bm, bn; double step, alone; };
-    // Blocks of one worker.
-    uint64_t blocks32(uint32_t q, uint32_t bm, uint32_t bn, uint64_t splits, uint64_t piece) const
-    {
-        if (rows_of_k) return ceil_div(M, bm) * ceil_div(N, bn) * std::max<uint64_t>(1, ceil_div(rows[q], piece));
-        return ceil_div(rows[q], bm) * ceil_div(N, bn) * splits;
-    }
-    Cut tiles32() const
+    const Cut& tiles32() const { return once(tiles32_, [&] { return find32(); }); }
+    Cut find32() const
     {
         static const Tile list[] = {{64, 64, 0.42, 0.47}, {32, 64, 0.24, 0.47}, {32, 32, 0.135, 0.16}, {16, 64, 0.18, 0.18}, {64, 16, 0.18, 0.18}};
         const uint64_t steps = ceil_div(K, 32);
-        double results = 0;
-        for (uint32_t q = 0; q < W; ++q) results += (double)(rows_of_k ? M : rows[q]) * (double)N;
         Cut b{};
         for (const Tile& t : list) {
-            // tiles of all workers, and the steps of all tiles where nothing is cut
-            uint64_t tiles = 0, all = 0;
-            for (uint32_t q = 0; q < W; ++q) {
-                const uint64_t n = rows_of_k ? ceil_div(M, t.bm) * ceil_div(N, t.bn) : ceil_div(rows[q], t.bm) * ceil_div(N, t.bn);
-                tiles += n;
-                all += n * (rows_of_k ? std::max<uint64_t>(1, ceil_div(rows[q], 32)) : steps);
-            }
+            const uint64_t all = steps_of_all(t.bm, t.bn, 32), tiles = rows_of_k ? W * ceil_div(M, t.bm) * ceil_div(N, t.bn) : all / std::max<uint64_t>(1, steps);
             const double area = t.bm * t.bn / 4096.0, read = (double)all * (t.bm + t.bn) * 128.0 / 18e6;
             uint64_t last = 0;
             for (const uint64_t want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48}) {
@@ -353,15 +361,41 @@ struct Product {
         }
         return b;
     }
+    // The blocks of every worker: only those that have work.
+    uint64_t number(const Cut& c, GemmArgs& a) const
+    {
+        uint64_t blocks = 0;
+        a.spread = uneven;
+        const uint64_t across = ceil_div(N, c.bn), down = ceil_div(M, c.bm);
+        for (uint32_t q = 0; q < W; ++q) {
+            a.first[q] = (uint32_t)blocks;
+            blocks += across * (rows_of_k ? down * std::max<uint64_t>(1, ceil_div(rows[q], c.piece)) : ceil_div(rows[q], c.bm) * c.splits);
+        }
+        for (uint32_t q = W; q <= MAXW_T; ++q) a.first[q] = (uint32_t)blocks;
+        a.blocks = (uint32_t)blocks;
+        a.each = (uint32_t)(blocks / W);
+        for (uint32_t q = 1; q < W; ++q)
+            if (a.first[q] != q * a.each) a.each = 0;
+        return blocks;
+    }
     // ... of rows that no vector fits in
     bool narrow() const { return std::min(N, rows_of_k ? M : K) < 4; }
-    bool few() const { return es == 2 && !rows_of_k && M <= 64 && ceil_div(N, 16) * W >= 64; }
+    bool few() const { return es == 2 && forward && M <= 64 && ceil_div(N, 16) * W >= 64; }
     static uint64_t bytes(const Cut& c, const Product& p) { return c.splits > 1 ? p.W * c.splits * p.M * p.N * 4 : 0; }
     uint64_t ws() const
     {
+        if (few()) return 0;
         if (es == 2) return std::max(bytes(elements(), *this), bytes(copies(), *this));
         return bytes(narrow() ? elements() : tiles32(), *this);
     }
+
+private:
+    template <class F> static const Cut& once(Cut& c, F&& f)
+    {
+        if (!c.bm) c = f();
+        return c;
+    }
+    mutable Cut copies_{}, elements_{}, tiles32_{};
 };
 
 // What a grid can number, whichever the tile; asked before a call's first launch.
@@ -386,6 +420,13 @@ template <bool AK, bool BK> int staging(const Call& c, const GemmArgs& a, const 
     return p.es == 2 ? std::max(of(a.a, a.lda, AK ? p.M : p.K), of(a.b, a.ldb, BK ? p.N : p.K)) : 2;
 }
 
+// A grid of so many blocks: one dimension numbers 2^32 threads.
+dim3 over_two(uint64_t blocks)
+{
+    constexpr uint64_t ACROSS = 1u << 20;
+    return dim3((uint32_t)std::min(blocks, ACROSS), (uint32_t)ceil_div(blocks, ACROSS));
+}
+
 // The second launch of a product whose sum was cut.
 template <class T, int EPI> int joined(Call& c, const GemmArgs& a, const Product& p)
 {
@@ -405,21 +446,12 @@ template <bool AK, bool BK, int EPI> int product(Call& c, GemmArgs a, const Prod
     a.partial = static_cast<float*>(ws);
     a.splits = 1;
     if (dtype == SLIMDP_F32 && !p.narrow()) {
-        const Product::Cut cut = p.tiles32();
+        const Product::Cut& cut = p.tiles32();
         a.splits = (uint32_t)cut.splits;
         a.k_split = (uint32_t)cut.piece;
-        uint64_t blocks = 0;
-        for (uint32_t q = 0; q < MAXW_T; ++q) {
-            a.first[q] = (uint32_t)blocks;
-            if (q < c.W) blocks += p.blocks32(q, cut.bm, cut.bn, cut.splits, cut.piece);
-        }
-        a.first[MAXW_T] = (uint32_t)blocks;
-        constexpr uint64_t ACROSS = 1u << 20;
+        const uint64_t blocks = p.number(cut, a);
         auto launch = [&](auto kernel) {
-            c.launched("k_gemm32", [&] {
-                const dim3 grid((uint32_t)std::min(blocks, ACROSS), (uint32_t)ceil_div(blocks, ACROSS));
-                hipLaunchKernelGGL(kernel, grid, dim3(256), 0, c.v.stream, a);
-            });
+            c.launched("k_gemm32", [&] { hipLaunchKernelGGL(kernel, over_two(blocks), dim3(256), 0, c.v.stream, a); });
         };
         if (cut.bm == 64 && cut.bn == 64) launch(k_gemm32<AK, BK, EPI, 64, 64, 2, 2>);
         else if (cut.bm == 32 && cut.bn == 64) launch(k_gemm32<AK, BK, EPI, 32, 64, 1, 4>);
@@ -447,15 +479,15 @@ template <bool AK, bool BK, int EPI> int product(Call& c, GemmArgs a, const Prod
         }
     }
     const int stage = staging<AK, BK>(c, a, p);
-    const Product::Cut cut = stage < 2 ? p.copies() : p.elements();
+    const Product::Cut& cut = stage < 2 ? p.copies() : p.elements();
     a.splits = (uint32_t)cut.splits;
     a.k_split = (uint32_t)cut.piece;
-    const dim3 grid((uint32_t)cut.tiles, 1, c.W * a.splits);
+    const uint64_t blocks = p.number(cut, a);
     with_type(dtype, [&](auto z) {
         typedef decltype(z) T;
         if constexpr (sizeof(T) == 2) {
             auto launch = [&](auto kernel) {
-                c.launched("k_gemm_tiles", [&] { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, c.v.stream, a); });
+                c.launched("k_gemm_tiles", [&] { hipLaunchKernelGGL(kernel, over_two(blocks), dim3(256), 0, c.v.stream, a); });
             };
             if (stage == 0 && cut.bm == 256) launch(k_gemm_tiles<T, AK, BK, EPI, 256, 256, 2, 2, 1, true>);
             else if (stage == 0) launch(k_gemm_tiles<T, AK, BK, EPI, 128, 128, 2, 2, 2, true>);
@@ -463,7 +495,9 @@ template <bool AK, bool BK, int EPI> int product(Call& c, GemmArgs a, const Prod
             else if (stage == 1) launch(k_gemm_tiles<T, AK, BK, EPI, 128, 128, 2, 2, 2, false>);
         }
         if (stage == 2)
-            c.launched("k_gemm", [&] { hipLaunchKernelGGL((k_gemm<T, AK, BK, EPI>), grid, dim3(256), 0, c.v.stream, a); });
+            c.launched("k_gemm", [&] {
+                hipLaunchKernelGGL((k_gemm<T, AK, BK, EPI>), dim3((uint32_t)cut.tiles, 1, c.W * a.splits), dim3(256), 0, c.v.stream, a);
+            });
         joined<T, EPI>(c, a, p);
     });
     return c.rc;
@@ -471,15 +505,15 @@ template <bool AK, bool BK, int EPI> int product(Call& c, GemmArgs a, const Prod
 
 Product forward_product(uint32_t W, const uint64_t* rows, uint64_t in, uint64_t out, size_t es)
 {
-    return {most_rows(W, rows), out, in, W, rows, es, false};
+    return Product(most_rows(W, rows), out, in, W, rows, es, 0);
 }
 Product input_product(uint32_t W, const uint64_t* rows, uint64_t in, uint64_t out, size_t es)
 {
-    return {most_rows(W, rows), in, out, W, rows, es, false};
+    return Product(most_rows(W, rows), in, out, W, rows, es, 1);
 }
 Product weight_product(uint32_t W, const uint64_t* rows, uint64_t in, uint64_t out, size_t es)
 {
-    return {out, in, most_rows(W, rows), W, rows, es, true};
+    return Product(out, in, most_rows(W, rows), W, rows, es, 2);
 }
 
 }  // namespace

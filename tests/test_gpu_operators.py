@@ -1130,3 +1130,43 @@ def test_products_in_binary32_keep_up_with_the_elementary_form(R, K, N, what):
     a, b = (sorted(p[i] for p in pairs)[4] for i in (0, 1))
     assert a < 1.5 * b + 20 * 5e-6, (a / 20 * 1e6, b / 20 * 1e6)                            # 5 us: a second launch from the host
     sd.close()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("rows,K,N", [([2300, 0, 1, 33], 136, 104), ([0, 0, 5, 0, 900], 40, 264), ([700, 31, 32, 33, 0, 1, 64, 65], 104, 72), ([4100, 0, 40, 1030], 1032, 2312),
+                                      ([0, 2500, 129], 2056, 520), ([70] * 32, 64, 48), ([1, 9000], 264, 264)])
+def test_products_of_uneven_workers(ctx, dtype, rows, K, N):
+    """Every tile, copied into the LDS and through registers, whole and in pieces, for workers of few rows beside others of many, or of none."""
+    for pad, shift in ((0, 0), (8, 8), (3, 1)):
+        check_workers(ctx, rows, K, N, TYPES[dtype], pad, shift)
+
+
+@pytest.mark.parametrize("what", ["forward", "dx", "dweight"])
+@pytest.mark.parametrize("rows", [[8192, 0, 0, 0, 0, 0, 0, 0], [0, 300, 7000, 892], [1, 4000, 4000, 63, 64, 64]])
+def test_products_take_the_time_of_their_rows_however_the_workers_share_them(rows, what):
+    """One worker with all the rows once took five to six times the time of eight with as many."""
+    import time
+    K, N, t = 2048, 2048, torch.bfloat16
+
+    def call(rows):
+        sd = binding.SlimDP(100, len(rows))
+        x, dz = [torch.randn(r, K, device="cuda").to(t) for r in rows], [torch.randn(r, N, device="cuda").to(t) for r in rows]
+        w = [torch.randn(N, K, device="cuda").to(t) for _ in rows]
+        y, dx, dw = [torch.empty_like(v) for v in dz], [torch.empty_like(v) for v in x], [torch.empty((N, K), device="cuda") for _ in rows]
+        return sd, {"forward": lambda: sd.linear(x, w, y=y), "dx": lambda: sd.linear_backward(dz, None, w, dx=dx, want_dweight=False),
+                    "dweight": lambda: sd.linear_backward(dz, x, None, dweight=dw, want_dx=False)}[what]
+    a, uneven = call(rows)
+    b, equal = call([1024] * 8 if len(rows) == 8 else [8192 // len(rows)] * len(rows))
+
+    def once(f):
+        t0 = time.perf_counter()
+        for _ in range(10):
+            f()
+        torch.cuda.synchronize()
+        return time.perf_counter() - t0
+    torch.cuda.synchronize()
+    once(uneven), once(equal)
+    pairs = [(once(uneven), once(equal)) for _ in range(9)]
+    got, want = (sorted(p[i] for p in pairs)[4] for i in (0, 1))
+    assert got < 1.6 * want, (got / 10 * 1e6, want / 10 * 1e6)
+    a.close(), b.close()
