@@ -188,7 +188,7 @@ __global__ __launch_bounds__(256) void k_norm_back_rows(NormBackArgs a)
 // grid (blocks, workers)
 struct NormBackSums {
     OutTab dweight, dbias;
-    float* partial;              // [worker][block][2][cols]; nullptr: one block a worker
+    float* partial;              // [worker][block][2][cols], of blocks that have rows; nullptr: one block a worker
     int accumulate;
 };
 template <class T, int TPR, int NC, int BT, int NT>
@@ -199,6 +199,7 @@ __global__ __launch_bounds__(BT) void k_norm_back(NormBackArgs a, NormBackSums o
     __shared__ float slots[2][2][BT / 64];
     __shared__ float meet[ROUNDS > 1 ? 2 : 1][ROUNDS > 1 ? WIDTH + TPR : 1];      // the last TPR: the elements behind the vectors
     const uint32_t q = blockIdx.y, rows = a.rows.n[q], cols = a.cols;
+    if (blockIdx.x * GROUPS >= rows && blockIdx.x) return;          // the whole block has no row; the first one of an empty worker writes zeros
     const uint32_t lane = threadIdx.x % TPR, group = threadIdx.x / TPR, step = gridDim.x * GROUPS;
     const T* dy = static_cast<const T*>(a.dy.p[q]);
     const T* x = static_cast<const T*>(a.x.p[q]);
@@ -501,7 +502,7 @@ struct ColumnSumArgs {
     const float* partial;
     OutTab out0, out1;
     RowTab rows;
-    uint32_t cols, slab, slabs, arrays;   // slab 0: every worker has all the slabs
+    uint32_t cols, slab, slabs, arrays;   // a worker has as many slabs as it has times `slab` rows, `slabs` at most
     int accumulate;
 };
 template <uint32_t SL>
@@ -510,7 +511,7 @@ __global__ __launch_bounds__(16 * SL) void k_column_sums(ColumnSumArgs a)
     __shared__ float part[SL][17];
     const uint32_t q = blockIdx.z, arr = blockIdx.y, tx = threadIdx.x & 15u, ty = threadIdx.x >> 4;
     const uint32_t c = blockIdx.x * 16 + tx;
-    const uint32_t n = a.slab ? max(1u, (a.rows.n[q] + a.slab - 1) / a.slab) : a.slabs;
+    const uint32_t n = min(a.slabs, max(1u, (a.rows.n[q] + a.slab - 1) / a.slab));
     const float* from = a.partial + ((size_t)q * a.slabs * a.arrays + arr) * a.cols + c;
     const size_t step = (size_t)a.arrays * a.cols;
     float s = 0.0f;

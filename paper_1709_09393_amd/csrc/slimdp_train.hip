@@ -180,6 +180,14 @@ bool shape_ok(uint32_t n_workers, const uint64_t* rows)
     return n_workers && n_workers <= SLIMDP_MAX_WORKERS && rows && most_rows(n_workers, rows) <= SLIMDP_MAX_ROWS;
 }
 
+// Workers that the rows would make if all had as many as the largest: what a launch's blocks are shared between (a worker without rows needs none).
+uint64_t crowd(uint32_t n_workers, const uint64_t* rows)
+{
+    uint64_t all = 0;
+    for (uint32_t q = 0; q < n_workers; ++q) all += rows[q];
+    return std::max<uint64_t>(1, ceil_div(all, std::max<uint64_t>(1, most_rows(n_workers, rows))));
+}
+
 // Vectors that a block of the sums over rows takes of a row.
 uint32_t column_lanes(uint64_t cols, size_t es)
 {
@@ -188,16 +196,16 @@ uint32_t column_lanes(uint64_t cols, size_t es)
 }
 // Rows of a slab of the sums over rows: as many slabs as give the chip eight blocks a compute unit (of 256), of four rows or more for
 // every group of a block's threads.
-uint64_t slab_rows(uint64_t most, uint32_t W, uint64_t cols, size_t es)
+uint64_t slab_rows(uint32_t W, const uint64_t* rows, uint64_t cols, size_t es)
 {
     const uint32_t lx = column_lanes(cols, es);
-    const uint64_t across = ceil_div(cols, lx * (16 / es)) * W;
+    const uint64_t most = most_rows(W, rows), across = ceil_div(cols, lx * (16 / es)) * crowd(W, rows);
     const uint64_t slabs = std::max<uint64_t>(1, std::min<uint64_t>(2048 / across, ceil_div(most, 4 * 256 / lx)));
     return std::max<uint64_t>(1, ceil_div(most, slabs));
 }
-uint64_t column_ws(uint64_t most, uint32_t W, uint64_t cols, size_t es, int arrays)
+uint64_t column_ws(uint32_t W, const uint64_t* rows, uint64_t cols, size_t es, int arrays)
 {
-    const uint64_t slabs = ceil_div(most, slab_rows(most, W, cols, es));
+    const uint64_t slabs = ceil_div(most_rows(W, rows), slab_rows(W, rows, cols, es));
     return slabs <= 1 ? 0 : W * slabs * arrays * cols * 4;
 }
 
@@ -205,13 +213,13 @@ uint64_t column_ws(uint64_t most, uint32_t W, uint64_t cols, size_t es, int arra
 // the chip; four rows a group at least, so that the sums that the blocks write are few beside the rows).  tpr 0: rows too long to
 // be held beside their sums, two passes.
 struct NormBackShape { uint32_t tpr, block; uint64_t blocks; };
-NormBackShape norm_back_shape(uint64_t most, uint32_t W, uint64_t cols, size_t es)
+NormBackShape norm_back_shape(uint32_t W, const uint64_t* rows, uint64_t cols, size_t es)
 {
-    const uint64_t n = ceil_div(cols, 16 / es);
+    const uint64_t most = most_rows(W, rows), n = ceil_div(cols, 16 / es);
     const uint32_t tpr = n <= 8 ? 8 : n <= 16 ? 16 : n <= 32 ? 32 : n <= 128 ? 64 : n <= 512 ? 256 : n <= 1024 ? 512 : n <= 2048 ? 1024 : 0;
     if (!tpr) return {0, 0, 0};
     const uint32_t block = tpr <= 64 ? 256 : 1024, groups = block / tpr;
-    const uint64_t fill = std::max<uint64_t>(1, (block == 256 ? 1024 : 256) / W);
+    const uint64_t fill = std::max<uint64_t>(1, (block == 256 ? 1024 : 256) / crowd(W, rows));
     return {tpr, block, std::max<uint64_t>(1, std::min(fill, ceil_div(most, 4 * groups)))};
 }
 
@@ -229,7 +237,7 @@ template <bool NORM> int column_grads(Call& c, ColumnArgs a, uint32_t dtype, int
 {
     constexpr int ARR = NORM ? 2 : 1;
     a.rows = c.tab;
-    a.slab = (uint32_t)slab_rows(c.most, c.W, a.cols, c.esize);
+    a.slab = (uint32_t)slab_rows(c.W, c.rows, a.cols, c.esize);
     a.slabs = (uint32_t)std::max<uint64_t>(1, ceil_div(c.most, a.slab));
     a.partial = sums && a.slabs > 1 ? static_cast<float*>(ws) : nullptr;
     with_type(dtype, [&](auto z) {
@@ -548,7 +556,7 @@ int slimdp_layer_norm(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* rows,
         // eight blocks of 256 threads a compute unit (of 256), a block's next row under way while it sums the present one
         auto launch = [&](auto kernel, auto kernel_nt, uint32_t tpr) {
             const uint32_t block = std::max(tpr, 256u), groups = block / tpr;
-            const uint64_t want = ceil_div(c.most, groups), cap = std::max<uint64_t>(1, 2048 * 256 / block / c.W);
+            const uint64_t want = ceil_div(c.most, groups), cap = std::max<uint64_t>(1, 2048 * 256 / block / crowd(c.W, rows));
             c.launched("k_norm", [&] {
                 const dim3 grid((uint32_t)std::min(want, cap), c.W);
                 if (nt) hipLaunchKernelGGL(kernel_nt, grid, dim3(block), 0, c.v.stream, a);
@@ -577,10 +585,9 @@ uint64_t slimdp_layer_norm_workspace_bytes(uint32_t n_workers, const uint64_t* r
 {
     if (!shape_ok(n_workers, rows) || cols == 0 || cols > SLIMDP_MAX_NORM_COLS || dtype > SLIMDP_BF16) return 0;
     const size_t es = dtype == SLIMDP_F32 ? 4 : 2;
-    const uint64_t most = most_rows(n_workers, rows);
-    const NormBackShape s = norm_back_shape(most, n_workers, cols, es);
+    const NormBackShape s = norm_back_shape(n_workers, rows, cols, es);
     if (s.tpr) return s.blocks > 1 ? n_workers * s.blocks * 2 * cols * 4 : 0;
-    return column_ws(most, n_workers, cols, es, 2);
+    return column_ws(n_workers, rows, cols, es, 2);
 }
 
 int slimdp_layer_norm_backward(slimdp_ctx* ctx, uint32_t n_workers, const uint64_t* rows, uint64_t cols, uint32_t dtype,
@@ -612,7 +619,7 @@ int slimdp_layer_norm_backward(slimdp_ctx* ctx, uint32_t n_workers, const uint64
     if (!c.ok()) return c.rc;
     const NormBackArgs a{c.in(dy), c.in(x), c.in(weight), c.in(mean), c.in(rstd), c.out(dx), c.tab, lddy, ldx, lddx, (uint32_t)cols};
     const int accumulate = (flags & SLIMDP_GRAD_ACCUMULATE) != 0;
-    const NormBackShape shape = norm_back_shape(c.most, c.W, cols, c.esize);
+    const NormBackShape shape = norm_back_shape(c.W, rows, cols, c.esize);
     if (shape.tpr) {
         if (!sums && c.most == 0) return c.rc;
         const bool nt = c.bytes(cols, 3) > STREAM_BYTES;
@@ -639,7 +646,7 @@ int slimdp_layer_norm_backward(slimdp_ctx* ctx, uint32_t n_workers, const uint64
             else SLIMDP_NORM_BACK(1024, 2, 1024);
 #undef SLIMDP_NORM_BACK
         });
-        if (c.ok() && o.partial) column_sums(c, ColumnSumArgs{o.partial, o.dweight, o.dbias, c.tab, (uint32_t)cols, 0, (uint32_t)shape.blocks, 2, accumulate});
+        if (c.ok() && o.partial) column_sums(c, ColumnSumArgs{o.partial, o.dweight, o.dbias, c.tab, (uint32_t)cols, shape.block / shape.tpr, (uint32_t)shape.blocks, 2, accumulate});
         return c.rc;
     }
     if (sums) {      // before dx, which may overwrite dy or x
@@ -666,9 +673,8 @@ uint64_t slimdp_linear_workspace_bytes(uint32_t n_workers, const uint64_t* rows,
         pass > SLIMDP_LINEAR_BACKWARD)
         return 0;
     const size_t es = dtype == SLIMDP_F32 ? 4 : 2;
-    const uint64_t most = most_rows(n_workers, rows);
     if (pass == SLIMDP_LINEAR_FORWARD) return forward_product(n_workers, rows, in, out, es).ws();
-    if (pass == SLIMDP_LINEAR_EPILOGUE_BACKWARD) return column_ws(most, n_workers, out, es, 1);
+    if (pass == SLIMDP_LINEAR_EPILOGUE_BACKWARD) return column_ws(n_workers, rows, out, es, 1);
     return std::max(input_product(n_workers, rows, in, out, es).ws(), weight_product(n_workers, rows, in, out, es).ws());
 }
 

@@ -1170,3 +1170,79 @@ def test_products_take_the_time_of_their_rows_however_the_workers_share_them(row
     got, want = (sorted(p[i] for p in pairs)[4] for i in (0, 1))
     assert got < 1.6 * want, (got / 10 * 1e6, want / 10 * 1e6)
     a.close(), b.close()
+
+
+def device_normal(seed, rows, cols, t, sigma=1.0, mean=0.0):
+    """Large matrices are drawn where they are used."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return torch.empty((rows, cols), device="cuda").normal_(mean, sigma, generator=g).to(t)
+
+
+def check_norm(ctx, rows, cols, t):
+    """Layer norm and its backward pass of several workers against 64 bits, with and without each other's outputs."""
+    x = [device_normal(q, r, cols, t, 1.5, 0.7) for q, r in enumerate(rows)]
+    dy = [device_normal(q + 100, r, cols, t, 0.3) for q, r in enumerate(rows)]
+    mk = Maker(cols)
+    w, b = [mk.vec(cols, 0.3, 1.0) for _ in rows], [mk.vec(cols, 0.3) for _ in rows]
+    y, mean, rstd = ctx.layer_norm(x, w, b)
+    dx, gw, gb = ctx.layer_norm_backward(dy, x, w, mean, rstd)
+    _, gw2, gb2 = ctx.layer_norm_backward(dy, x, w, mean, rstd, want_dx=False)
+    ctx.synchronize()
+    for q, r in enumerate(rows):
+        what, sw, sb, tw, tb = f"{t} {rows} x {cols} worker {q} ", 0.0, 0.0, 1e-30, 1e-30
+        for a in range(0, r, 4096):
+            part = slice(a, min(r, a + 4096))
+            xd, dyd = x[q][part].double(), dy[q][part].double()
+            ref, rm, rr, ty, tm, tr = norm_tolerance(xd, w[q].double(), b[q].double(), 1e-5, t)
+            close(mean[q][part], rm, tm + tiny(torch.float32), what + "mean")
+            close(rstd[q][part], rr, tr, what + "rstd")
+            close(y[q][part], ref, ty, what + "y")
+            ref, e, xh, exh = norm_back_reference(dyd, xd, w[q].double(), mean[q][part].double(), rstd[q][part].double())
+            close(dx[q][part], ref, u(t) * ref.abs() + 1.01 * e + tiny(t), what + "dx")
+            n = (r + 8) * F
+            sw, sb = sw + (dyd * xh).sum(0), sb + dyd.sum(0)
+            tw, tb = tw + n * (dyd.abs() * (xh.abs() + exh)).sum(0) + (dyd.abs() * exh).sum(0), tb + n * dyd.abs().sum(0)
+        for got_w, got_b in ((gw[q], gb[q]), (gw2[q], gb2[q])):
+            close(got_w, sw if r else torch.zeros_like(got_w), tw, what + "dweight")
+            close(got_b, sb if r else torch.zeros_like(got_b), tb, what + "dbias")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,cols", [([3000, 0, 1, 17, 0, 0, 0, 0], 96), ([0, 2500], 2048), ([1, 900, 2], 4099), ([0, 0, 400, 1], 20000), ([700, 3], 33000),
+                                       ([40] * 32, 130), ([9000, 9], 24)])
+def test_layer_norm_of_uneven_workers(ctx, dtype, rows, cols):
+    """Rows of one pass and of two, blocks without rows, sums of workers that have a block or two beside others that have hundreds."""
+    check_norm(ctx, rows, cols, TYPES[dtype])
+
+
+@pytest.mark.parametrize("what", ["norm", "norm_back", "act_back"])
+@pytest.mark.parametrize("rows", [[16384, 0, 0, 0, 0, 0, 0, 0], [0, 0, 16000, 100, 100, 100, 84, 0]])
+def test_sums_over_rows_take_the_time_of_their_rows_however_the_workers_share_them(rows, what):
+    """One worker with all the rows once had an eighth of the chip for layer norm's backward pass, and took five times the time."""
+    import time
+    D, t = 4096, torch.bfloat16
+
+    def call(rows):
+        sd = binding.SlimDP(100, len(rows))
+        x, dy = [device_normal(q, r, D, t) for q, r in enumerate(rows)], [device_normal(q + 9, r, D, t) for q, r in enumerate(rows)]
+        w, y = [torch.ones(D, device="cuda") for _ in rows], [torch.empty_like(v) for v in x]
+        mean, rstd = [torch.zeros(r, device="cuda") for r in rows], [torch.ones(r, device="cuda") for r in rows]
+        a, b = [torch.empty(D, device="cuda") for _ in rows], [torch.empty(D, device="cuda") for _ in rows]
+        return sd, {"norm": lambda: sd.layer_norm(x, w, w, y=y, mean=mean, rstd=rstd),
+                    "norm_back": lambda: sd.layer_norm_backward(dy, x, w, mean, rstd, dx=y, dweight=a, dbias=b),
+                    "act_back": lambda: sd.linear_epilogue_backward(dy, x, "gelu", dz=y, dbias=a)}[what]
+    (a, uneven), (b, equal) = call(rows), call([2048] * 8)
+
+    def once(f):
+        t0 = time.perf_counter()
+        for _ in range(10):
+            f()
+        torch.cuda.synchronize()
+        return time.perf_counter() - t0
+    torch.cuda.synchronize()
+    once(uneven), once(equal)
+    pairs = [(once(uneven), once(equal)) for _ in range(9)]
+    got, want = (sorted(p[i] for p in pairs)[4] for i in (0, 1))
+    assert got < 1.8 * want, (got / 10 * 1e6, want / 10 * 1e6)
+    a.close(), b.close()
