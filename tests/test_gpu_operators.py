@@ -1246,3 +1246,92 @@ def test_sums_over_rows_take_the_time_of_their_rows_however_the_workers_share_th
     got, want = (sorted(p[i] for p in pairs)[4] for i in (0, 1))
     assert got < 1.8 * want, (got / 10 * 1e6, want / 10 * 1e6)
     a.close(), b.close()
+
+
+@pytest.mark.parametrize("rows,cols", [([30000], 40), ([140000, 3], 48), ([20000], 200), ([9000], 500), ([5000, 2600], 1000), ([6000], 1024), ([2100], 2100), ([2200, 2200], 4000),
+                                       ([700], 9000), ([1200], 16000), ([300], 30000), ([600], 65536)])
+def test_layer_norm_of_more_rows_than_blocks(ctx, rows, cols):
+    """Blocks that take a second and a third row, the next one under way, for every number of threads to a row; more than 128 and 512 blocks'
+    sums for the joining pass."""
+    for t in (torch.float32, torch.bfloat16):
+        check_norm(ctx, rows, cols, t)
+
+
+@pytest.mark.parametrize("dtype,rows,cols", [("bf16", [30000, 10000], 2048), ("f16", [20000], 4101), ("f32", [40000], 1000), ("f32", [2500], 20000), ("bf16", [4300], 33000),
+                                             ("bf16", [900000], 100)])
+def test_layer_norm_of_streams_that_no_cache_holds(ctx, dtype, rows, cols):
+    """More than 256 MB: the variants that pass the caches by."""
+    assert sum(rows) * cols * 2 * (4 if dtype == "f32" else 2) > 256 << 20
+    check_norm(ctx, rows, cols, TYPES[dtype])
+
+
+def check_epilogue_backward(ctx, rows, out, t, act):
+    dy = [device_normal(q, r, out, t, 0.3) for q, r in enumerate(rows)]
+    z = [device_normal(q + 50, r, out, t) for q, r in enumerate(rows)]
+    dz, db = ctx.linear_epilogue_backward(dy, z, act, dz=[torch.empty_like(v) for v in dy])
+    ctx.synchronize()
+    for q, r in enumerate(rows):
+        what, total, tb = f"{t} {rows} x {out} {act} worker {q} ", torch.zeros(out, dtype=torch.float64, device="cuda"), 1e-30
+        for a in range(0, r, 1 << 16):
+            part = slice(a, min(r, a + (1 << 16)))
+            dyd = dy[q][part].double()
+            ref = dyd * act_slope(z[q][part].double(), act)
+            e = dyd.abs() * 64 * F
+            close(dz[q][part], ref, u(t) * ref.abs() + e + tiny(t), what + "dz")
+            total, tb = total + ref.sum(0), tb + (r + 8) * F * (ref.abs() + e).sum(0) + e.sum(0)
+        close(db[q], total, tb, what + "dbias")
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("dtype,rows,out", [("bf16", [200000], 48), ("f32", [70000, 5, 0], 33), ("f16", [9000, 0, 1], 300), ("f32", [0, 3000], 1001), ("bf16", [45000], 1111),
+                                            ("f32", [30000], 1000), ("bf16", [1500000], 33)])
+def test_epilogue_backward_of_many_and_uneven_rows(ctx, act, dtype, rows, out):
+    """More than 128 and 512 slabs, slabs of one worker alone, and streams of more than 256 MB."""
+    check_epilogue_backward(ctx, rows, out, TYPES[dtype], act)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,V,top", [([70000, 5], 100, 7), ([66000], 130, 300)])
+def test_distill_of_more_rows_than_blocks(ctx, dtype, rows, V, top):
+    """A block's second row: its lists, counts and sums begin anew."""
+    t, mk = TYPES[dtype], Maker(18)
+    logits = [device_normal(q, r, V, t, 2.0) for q, r in enumerate(rows)]
+    idx = [torch.from_numpy(mk.g.integers(0, V, (r, top)).astype(np.int32)).cuda() for r in rows]          # entries that appear twice among them
+    for i, r in zip(idx, rows):
+        keep = torch.from_numpy(mk.g.integers(0, top + 1, r)).cuda()
+        i[torch.arange(top, device="cuda")[None] >= keep[:, None]] = -1
+    val = [device_normal(q + 9, r, top, torch.float32, 2.0, 5.0) for q, r in enumerate(rows)]
+    wt = [torch.from_numpy(mk.g.random(r).astype(np.float32)).cuda() for r in rows]
+    wt[0][3::7] = 0.0
+    loss, lse, d = ctx.distill_loss(logits, idx, val, 1.5, row_weight=wt)
+    only, lse2, _ = ctx.distill_loss(logits, idx, val, 1.5, row_weight=wt, want_grad=False)
+    ctx.synchronize()
+    for q in range(len(rows)):
+        rl, re, rd, tl, te, td = distill_reference(logits[q], idx[q], val[q], 1.5, wt[q], t)
+        close(loss[q], rl, tl, f"loss {q}")
+        close(only[q], rl, tl, f"loss alone {q}")
+        close(lse[q], re, te, f"lse {q}")
+        close(lse2[q], re, te, f"lse alone {q}")
+        close(d[q], rd, td, f"dlogits {q}")
+
+
+@pytest.mark.parametrize("dtype,rows,V", [("f32", 70000, 500), ("bf16", 20000, 4000), ("f16", 9000, 8000), ("f32", 4500, 8000), ("bf16", 3000, 30000), ("bf16", 1100, 65000),
+                                          ("f32", 600, 65536), ("bf16", 700, 131072), ("f32", 500, 100001), ("bf16", 500, 152064)])
+def test_distill_of_streams_that_no_cache_holds(ctx, dtype, rows, V):
+    """More than 256 MB of logits and gradients, every number of threads to a row."""
+    t, mk, top = TYPES[dtype], Maker(19), 12
+    assert rows * V * 2 * (4 if dtype == "f32" else 2) > 256 << 20
+    logits = device_normal(3, rows, V, t, 2.0)
+    idx, val = torch.from_numpy(mk.g.integers(0, V, (rows, top)).astype(np.int32)).cuda(), device_normal(4, rows, top, torch.float32, 2.0, 5.0)
+    wt = torch.ones(rows, device="cuda")
+    loss, lse, d = ctx.distill_loss([logits], [idx], [val], 2.0)
+    only, _, _ = ctx.distill_loss([logits], [idx], [val], 2.0, want_grad=False)
+    ctx.synchronize()
+    step = max(1, (1 << 26) // V)
+    for a in range(0, rows, step):
+        part = slice(a, min(rows, a + step))
+        rl, re, rd, tl, te, td = distill_reference(logits[part], idx[part], val[part], 2.0, wt[part], t)
+        close(loss[0][part], rl, tl, f"loss {a}")
+        close(only[0][part], rl, tl, f"loss alone {a}")
+        close(lse[0][part], re, te, f"lse {a}")
+        close(d[0][part], rd, td, f"dlogits {a}")
