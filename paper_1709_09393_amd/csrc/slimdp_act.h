@@ -9,8 +9,9 @@ enum : int { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_GELU_TANH = 3, ACT_SI
 constexpr float LOG2E = 1.4426950408889634f;
 
 // exp(-a^2 / 2) and the normal distribution function at -a, for a >= 0.  The latter is exp(-a^2 / 2) times a function that varies
-// slowly: a polynomial of degree 8 in 1 / (1 + 0.3 a), fitted here over a <= 14 (weighted least squares until the largest relative error
-// stopped falling: 5.8e-8, 4e-7 evaluated in binary32; behind 14 the exponential is zero in binary32).  Twenty instructions, where
+// slowly: a polynomial of degree 8 in 1 / (1 + 0.3 a), fitted here over a <= 14 by weighted least squares.  With the constants as they stand,
+// rounded to binary32, it is off by 9.6e-8 of the value at most, and by 4.1e-7 where it is evaluated in binary32; behind 14 the exponential is
+// zero in binary32.  The exponential adds a^2 / 2 times three roundings of its argument (1e-5 of the value at a = 12).  Twenty instructions, where
 // the library's complementary error function takes more time than the memory this work waits for.
 __device__ __forceinline__ float normal_tail(float a, float& density)
 {

@@ -1335,3 +1335,28 @@ def test_distill_of_streams_that_no_cache_holds(ctx, dtype, rows, V):
         close(only[0][part], rl, tl, f"loss alone {a}")
         close(lse[0][part], re, te, f"lse {a}")
         close(d[0][part], rd, td, f"dlogits {a}")
+
+
+@pytest.mark.parametrize("act,lowest", [("gelu", -12.5), ("gelu_tanh", -8.0), ("silu", -80.0)])
+def test_activations_of_negative_arguments_relative_to_their_value(ctx, act, lowest):
+    """Where the value is far smaller than its argument.  An exponential of an argument w that was made with n roundings is off by n F |w| of
+    itself: gelu 3 of z^2 / 2, gelu_tanh 7 of u, silu 2 of z; the factor beside gelu's is off by 4e-7, and six more steps are a few
+    roundings each.  Slopes are sums of two terms of different sign: the same of their sizes."""
+    z = torch.linspace(lowest, -1e-3, 40001, dtype=torch.float64).float().cuda()
+    zd = z.double()
+    y, _ = ctx.linear([z[:, None].contiguous()], [torch.ones((1, 1), device="cuda")], None, act)
+    dz, _ = ctx.linear_epilogue_backward([torch.ones_like(z)[:, None]], [z[:, None].contiguous()], act)
+    ctx.synchronize()
+    u_ = 2 * math.sqrt(2 / math.pi) * (zd + 0.044715 * zd ** 3)
+    if act == "gelu":
+        value, e = zd * 0.5 * torch.erfc(-zd / math.sqrt(2.0)), 4e-7 + F * (1.5 * zd ** 2 + 12)
+        parts = (value / zd).abs() + (zd * torch.exp(-zd ** 2 / 2) / math.sqrt(2 * math.pi)).abs()
+        slope = value / zd + zd * torch.exp(-zd ** 2 / 2) / math.sqrt(2 * math.pi)
+    else:
+        u_, factor = (u_, 2 * math.sqrt(2 / math.pi) * (1 + 0.134145 * zd ** 2)) if act == "gelu_tanh" else (zd, 1.0)
+        s = torch.exp(u_) / (1 + torch.exp(u_))
+        value, e = zd * s, F * ((7 if act == "gelu_tanh" else 2) * u_.abs() + 16)
+        slope = s + zd * s * (1 - s) * factor
+        parts = s + (zd * s * (1 - s) * factor).abs()
+    close(y[0][:, 0], value, e * value.abs(), act)
+    close(dz[0][:, 0], slope, (e + 16 * F) * parts, act + " slope")
