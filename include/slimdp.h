@@ -360,9 +360,10 @@ int slimdp_pull_local_step(slimdp_ctx* ctx, const float* w, uint64_t core_epoch,
 /* ---------------------------------------------------------------------------------- */
 
 /* The gradient that slimdp_local_step takes comes from a forward and a backward pass over a worker's mini-batch.  The calls
- * below are operators of such passes for models with layer norms, matrix products and a vocabulary: they read parameters
+ * below are operators of such passes for models with layer norms, matrix products and a vocabulary: they read binary32 parameters
  * from the workers' local models, serve all workers in one launch, and write every parameter's gradient in binary32 where
- * slimdp_local_step and slimdp_local_step_pack read it.
+ * slimdp_local_step and slimdp_local_step_pack read it.  A matrix of sixteen-bit weights is a copy of its binary32 part of the local model,
+ * made by the caller after every step or pull that changes it (the library rounds none).
  *  - rows [host, n_workers]: rows (tokens) of each worker's mini-batch, <= SLIMDP_MAX_ROWS; 0 is allowed, the worker's matrices
  *    may then be NULL, and its parameter gradients are written as sums over nothing.
  *  - dtype: SLIMDP_F32, SLIMDP_F16 or SLIMDP_BF16, the type of everything given as void.  Vectors of parameters and all
@@ -370,7 +371,8 @@ int slimdp_pull_local_step(slimdp_ctx* ctx, const float* w, uint64_t core_epoch,
  *  - A matrix is a [host table, n_workers] of [dev] row-major arrays, its rows ld elements apart (the same for all workers, at
  *    least the row's length); any alignment that an element may have.  Elements between rows are neither read nor written.
  *  - Sums, statistics and exponentials are binary32; results of a sixteen-bit type are rounded once, to nearest even.
- *    Every sum has an order that depends on the sizes alone: same inputs, same bits.
+ *    Every sum has an order that depends on the sizes alone (all workers' rows and the distances of rows among them, no addresses):
+ *    same inputs, same bits.
  *  - Outputs must not overlap inputs or each other, but for the cases each call names (the same array, the same ld).  Outputs of
  *    different workers are different arrays; inputs (weights among them) may be shared.
  *  - workspace [dev, aligned to 16 bytes]: scratch of at least the bytes that the *_workspace_bytes function gives for the same arguments

@@ -480,6 +480,7 @@ class SlimDP:
     # -- operators of LocalTrain ---------------------------------------------------------
     # Lists hold one tensor a worker: matrices [rows of the worker, columns] with consecutive columns, rows any distance apart (the
     # same for all workers); parameters of the local model and their gradients binary32 and contiguous (pieces of flat vectors).
+    # With accumulate, gradients of parameters are added to the arrays given for them, and none is made for those that are not given.
     def _layout(self, who: str, x: Sequence):
         """(rows of every worker, columns, dtype number, torch dtype) from a call's first list."""
         if x[0].dim() != 2:

@@ -1360,3 +1360,27 @@ def test_activations_of_negative_arguments_relative_to_their_value(ctx, act, low
         parts = s + (zd * s * (1 - s) * factor).abs()
     close(y[0][:, 0], value, e * value.abs(), act)
     close(dz[0][:, 0], slope, (e + 16 * F) * parts, act + " slope")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,K,N", [([300, 0, 17], 264, 136), ([2100], 1032, 2312), ([40], 520, 1040), ([5, 700], 1000, 96)])
+def test_bits_do_not_depend_on_addresses(ctx, dtype, rows, K, N):
+    """The same values at every alignment and distance of rows: copied into the LDS or through registers, vectors whole or broken, the same order of
+    every sum."""
+    t, first = TYPES[dtype], None
+    for pad, shift in ((0, 0), (8, 8), (3, 1), (0, 5)):
+        mk = Maker(35, pad, shift)
+        x, dz, w = [mk.normal(r, K, t) for r in rows], [mk.normal(r, N, t, 0.1) for r in rows], [mk.normal(N, K, t, 0.05) for _ in rows]
+        b, g = [mk.vec(N) for _ in rows], [mk.vec(K) for _ in rows]
+        idx, val = zip(*[teacher(mk, r, K, 9) for r in rows])
+        y, z = ctx.linear(x, w, b, "gelu", keep=True)
+        dx, dw = ctx.linear_backward(dz, x, w)
+        da, db = ctx.linear_epilogue_backward(dz, z, "silu")
+        n, mean, rstd = ctx.layer_norm(x, g, g)
+        dn, dg, dc = ctx.layer_norm_backward(x, x, g, mean, rstd)
+        loss, lse, dl = ctx.distill_loss(x, idx, val, 2.0)
+        ctx.synchronize()
+        out = [v.clone() for part in (y, z, dx, dw, da, db, n, mean, rstd, dn, dg, dc, loss, lse, dl) for v in part]
+        first = first or out
+        for i, (a, c) in enumerate(zip(first, out)):
+            assert torch.equal(a, c), (pad, shift, i)
