@@ -80,13 +80,18 @@ template <bool KROWS, uint32_t X> struct Tile32 {
 // Reads, copies and loads are put between the products one by one, and loads are made without a condition but in the last steps.  Operands
 // with rows of k stay as they lie (turning them over in registers on the way took a third of the time of the weight's gradient).
 //
+// LONG: every 256 of k the sums go over to a second set, so that a chain of additions is no longer than that (2048 x 4096 x 2048: error 3.0e-7 of
+// the result's size, 1.15e-6 in one chain, which is what a library product has).  The second set takes 16 registers of 64 x 64's
+// waves, three instead of four a SIMD: sums of 256 and less do without (8 x 40 x 1040 x 7692's weight gradient, which its stores bound,
+// 117 us instead of 127; 2048 x 4096 x 4096 the same either way).
+//
 // Bound by the matrix unit: 2048 x 4096 x 4096 515 us (133 TFLOP/s; a library product 465 to 530 on the same machines), 1024 x 1024 x 1024
 // 25 us (24).  Tiles are no larger than 64 x 64 because more blocks leave less of the last round empty (1529 x 832 x 3119: 92 us
 // with 128 x 64, 78 so), and narrower where the result is: 13,286 x 6638 x 16 80 us with 64 x 16, 155 with 64 x 64; 24 x 3592 x 4608 22 us
 // with 32 x 64.  Few rows are bound by memory, and so is what has few of k.
 // grid: a.blocks, over two dimensions where one does not number them
-template <bool AK, bool BK_, int EPI, uint32_t BM, uint32_t BN, uint32_t WM, uint32_t WN>
-__global__ __launch_bounds__(256, 4) void k_gemm32(GemmArgs a)
+template <bool AK, bool BK_, int EPI, uint32_t BM, uint32_t BN, uint32_t WM, uint32_t WN, bool LONG>
+__global__ __launch_bounds__(256, LONG && BM * BN == 4096 ? 3 : 4) void k_gemm32(GemmArgs a)
 {
     constexpr uint32_t MT = BM / WM, NT = BN / WN, FM = MT / 16, FN = NT / 16, BK = GEMM32_BK;
     typedef Tile32<AK, BM> TA;
@@ -110,11 +115,24 @@ __global__ __launch_bounds__(256, 4) void k_gemm32(GemmArgs a)
     const uint32_t k0 = min(Kall, split * a.k_split), K = min(Kall, k0 + a.k_split), steps = (K - k0 + BK - 1) / BK;
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
 
-    f32x4 acc[FM][FN];
+    f32x4 acc[FM][FN], sum[LONG ? FM : 1][LONG ? FN : 1];
+    auto carry = [&]() {
+        if constexpr (LONG)
+#pragma unroll
+            for (uint32_t i = 0; i < FM; ++i)
+#pragma unroll
+                for (uint32_t j = 0; j < FN; ++j) {
+                    sum[i][j] += acc[i][j];
+                    acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+                }
+    };
 #pragma unroll
     for (uint32_t i = 0; i < FM; ++i)
 #pragma unroll
-        for (uint32_t j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (uint32_t j = 0; j < FN; ++j) {
+            acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if constexpr (LONG) sum[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
     if (steps) {
         TA ta;
         TB tb;
@@ -204,12 +222,20 @@ __global__ __launch_bounds__(256, 4) void k_gemm32(GemmArgs a)
         for (; s + 5 < steps; s += 2) {
             step(s, c1, std::true_type{});
             step(s + 1, c0, std::true_type{});
+            if ((s & 6u) == 6u) carry();
         }
 #pragma unroll 1
         for (; s < steps; s += 2) {
             step(s, c1, std::false_type{});
             if (s + 1 < steps) step(s + 1, c0, std::false_type{});
         }
+    }
+    if constexpr (LONG) {
+        carry();
+#pragma unroll
+        for (uint32_t i = 0; i < FM; ++i)
+#pragma unroll
+            for (uint32_t j = 0; j < FN; ++j) acc[i][j] = sum[i][j];
     }
 #pragma unroll
     for (uint32_t i = 0; i < FM; ++i) {

@@ -461,11 +461,12 @@ template <bool AK, bool BK, int EPI> int product(Call& c, GemmArgs a, const Prod
         auto launch = [&](auto kernel) {
             c.launched("k_gemm32", [&] { hipLaunchKernelGGL(kernel, over_two(blocks), dim3(256), 0, c.v.stream, a); });
         };
-        if (cut.bm == 64 && cut.bn == 64) launch(k_gemm32<AK, BK, EPI, 64, 64, 2, 2>);
-        else if (cut.bm == 32 && cut.bn == 64) launch(k_gemm32<AK, BK, EPI, 32, 64, 1, 4>);
-        else if (cut.bm == 32) launch(k_gemm32<AK, BK, EPI, 32, 32, 2, 2>);
-        else if (cut.bm == 16) launch(k_gemm32<AK, BK, EPI, 16, 64, 1, 4>);
-        else launch(k_gemm32<AK, BK, EPI, 64, 16, 4, 1>);
+        if (cut.bm == 64 && cut.bn == 64 && std::min(cut.piece, p.K) <= 256) launch(k_gemm32<AK, BK, EPI, 64, 64, 2, 2, false>);
+        else if (cut.bm == 64 && cut.bn == 64) launch(k_gemm32<AK, BK, EPI, 64, 64, 2, 2, true>);
+        else if (cut.bm == 32 && cut.bn == 64) launch(k_gemm32<AK, BK, EPI, 32, 64, 1, 4, true>);
+        else if (cut.bm == 32) launch(k_gemm32<AK, BK, EPI, 32, 32, 2, 2, true>);
+        else if (cut.bm == 16) launch(k_gemm32<AK, BK, EPI, 16, 64, 1, 4, true>);
+        else launch(k_gemm32<AK, BK, EPI, 64, 16, 4, 1, true>);
         return joined<float, EPI>(c, a, p);
     }
     if constexpr (!AK && !BK) {

@@ -1384,3 +1384,22 @@ def test_bits_do_not_depend_on_addresses(ctx, dtype, rows, K, N):
         first = first or out
         for i, (a, c) in enumerate(zip(first, out)):
             assert torch.equal(a, c), (pad, shift, i)
+
+
+@pytest.mark.parametrize("K", [96, 777, 4096, 8192])
+@pytest.mark.parametrize("R,N", [(64, 64), (33, 1001), (2048, 512), (4000, 16)])
+def test_products_in_binary32_are_as_exact_as_short_chains(ctx, R, K, N):
+    """Root mean square error of products of random signs.  A rounding's square is (half a step)^2 / 3 on average, F^2 / 3 of the value's at
+    most; the k-th partial sum of a chain of n has the mean square k / n of the whole's, so a chain is off by F sqrt(n / 6) of its result.
+    Chains here hold 13 steps of 32 at most; K / 256 of them and up to 48 pieces are joined by chains likewise, and one more rounding."""
+    x, w = device_normal(1, R, K, torch.float32), device_normal(2, N, K, torch.float32)
+    y, _ = ctx.linear([x], [w])
+    dx, _ = ctx.linear_backward([x], None, [w.t().contiguous()], want_dweight=False)
+    _, dw = ctx.linear_backward([x.t().contiguous()], [w.t().contiguous()], None, want_dx=False)
+    ctx.synchronize()
+    ref = x.double() @ w.double().t()
+    size = float(ref.square().mean().sqrt())
+    bound = F * math.sqrt(min(K, 416) / 6 + (K / 256 + 48) / 6 + 1)
+    for what, got in (("forward", y[0]), ("dx", dx[0]), ("dweight", dw[0])):
+        err = float((got.double() - ref).square().mean().sqrt()) / size
+        assert err <= bound, (what, err, bound)
