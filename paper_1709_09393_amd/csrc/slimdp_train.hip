@@ -381,8 +381,8 @@ struct Product {
         }
         for (uint32_t q = W; q <= MAXW_T; ++q) a.first[q] = (uint32_t)blocks;
         a.blocks = (uint32_t)blocks;
-        a.each = (uint32_t)(blocks / W);
-        for (uint32_t q = 1; q < W; ++q)
+        a.each = a.first[1];
+        for (uint32_t q = 2; q <= W; ++q)
             if (a.first[q] != q * a.each) a.each = 0;
         return blocks;
     }

@@ -1403,3 +1403,11 @@ def test_products_in_binary32_are_as_exact_as_short_chains(ctx, R, K, N):
     for what, got in (("forward", y[0]), ("dx", dx[0]), ("dweight", dw[0])):
         err = float((got.double() - ref).square().mean().sqrt()) / size
         assert err <= bound, (what, err, bound)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [[64, 65], [128, 192], [128, 129], [256, 512], [16, 17], [1, 700], [64, 64, 200], [300, 300, 300, 1000], [0, 64], [64, 0], [64, 64, 0], [0, 0, 64, 128]])
+def test_workers_whose_numbers_of_tiles_begin_alike(ctx, dtype, rows):
+    """The last worker has a tile more, or none: blocks are not shared out as if all had the first one's number."""
+    for K, N in ((64, 48), (1024, 72)):
+        check_workers(ctx, rows, K, N, TYPES[dtype])
