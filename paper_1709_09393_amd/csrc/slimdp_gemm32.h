@@ -78,16 +78,17 @@ template <bool KROWS, uint32_t X> struct Tile32 {
 // wave of a 64 x 64 tile, so everything else has time beside it: a step's vectors are asked for three steps ahead, wait in registers for two,
 // and go to the other half of the LDS while a step is multiplied; fragments are read half a step ahead; one barrier a step, in its middle.
 // Reads, copies and loads are put between the products one by one, and loads are made without a condition but in the last steps.  Operands
-// with rows of k stay as they lie (turning them over in registers on the way took a third of the time of the weight's gradient).
+// with rows of k stay as they lie (a kernel that turned them over in registers took 741 us for the weight's gradient of 2048 x 4096 x 4096, this
+// one 524).
 //
-// LONG: every 256 of k the sums go over to a second set, so that a chain of additions is no longer than that (2048 x 4096 x 2048: error 3.0e-7 of
+// LONG: every 256 of k the sums go over to a second set, so that no chain of additions is longer than 13 steps (2048 x 4096 x 2048: error 3.0e-7 of
 // the result's size, 1.15e-6 in one chain, which is what a library product has).  The second set takes 16 registers of 64 x 64's
 // waves, three instead of four a SIMD: sums of 256 and less do without (8 x 40 x 1040 x 7692's weight gradient, which its stores bound,
 // 117 us instead of 127; 2048 x 4096 x 4096 the same either way).
 //
-// Bound by the matrix unit: 2048 x 4096 x 4096 515 us (133 TFLOP/s; a library product 465 to 530 on the same machines), 1024 x 1024 x 1024
+// Bound by the matrix unit: 2048 x 4096 x 4096 522 us (132 TFLOP/s; a library product 531 on that machine, 465 on another), 1024 x 1024 x 1024
 // 25 us (24).  Tiles are no larger than 64 x 64 because more blocks leave less of the last round empty (1529 x 832 x 3119: 92 us
-// with 128 x 64, 78 so), and narrower where the result is: 13,286 x 6638 x 16 80 us with 64 x 16, 155 with 64 x 64; 24 x 3592 x 4608 22 us
+// with 128 x 64, 78 so), and narrower where the result is: 13,286 x 6638 x 16 80 us with 64 x 16 (155 with the square tiles of an earlier kernel); 24 x 3592 x 4608 22 us
 // with 32 x 64.  Few rows are bound by memory, and so is what has few of k.
 // grid: a.blocks, over two dimensions where one does not number them
 template <bool AK, bool BK_, int EPI, uint32_t BM, uint32_t BN, uint32_t WM, uint32_t WN, bool LONG>
