@@ -360,7 +360,8 @@ __global__ __launch_bounds__(512) void k_gemm_few(GemmArgs a)
     epilogue4<T, EPI>(a, q, m, n, N, s);
 }
 
-// The pieces of split sums, added in order, and the epilogue.  grid (blocks, rows in turn, workers)
+// The pieces of split sums, added in order (eight asked for at a time, the last one again where there are fewer), and the epilogue.
+// grid (blocks, rows in turn, workers)
 template <class T, int EPI>
 __global__ __launch_bounds__(256) void k_gemm_join(GemmArgs a)
 {
@@ -371,11 +372,17 @@ __global__ __launch_bounds__(256) void k_gemm_join(GemmArgs a)
     const uint32_t pieces = a.k_is_rows ? max(1u, (a.rows.n[q] + a.k_split - 1) / a.k_split) : a.splits;
     for (uint32_t m = blockIdx.y; m < M; m += gridDim.y) {
         float s[4] = {0.f, 0.f, 0.f, 0.f};
-        for (uint32_t p = 0; p < pieces; ++p) {
-            float x[4];
-            load4(a.partial + (((size_t)q * a.splits + p) * a.M + m) * N + n, N - n, x);
+        const float* from = a.partial + (((size_t)q * a.splits) * a.M + m) * N + n;
+        const size_t step = (size_t)a.M * N;
+        for (uint32_t p = 0; p < pieces; p += 8) {
+            float x[8][4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[e] += x[e];
+            for (uint32_t i = 0; i < 8; ++i) load4(from + min(p + i, pieces - 1) * step, N - n, x[i]);
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (p + i < pieces) s[e] += x[i][e];
         }
         epilogue4<T, EPI>(a, q, m, n, N, s);
     }

@@ -342,9 +342,9 @@ struct Product {
     }
     // Binary32.  A block's step is 32 of k.  One block to a compute unit takes `alone` us for it, several share the unit at `step` each;
     // `begin` us a block of 64 x 64 for what is no step, 18 TB/s for what all blocks read together (the caches' rate), and where the sum
-    // is cut a second launch and the pieces' way to memory and back.  Fitted to the times of 4,100 products of 1 to 16,384 rows, 16 to 8192 in and
-    // out, forward and backward, one to eight workers, with every tile and 1 to 48 pieces: the cut that these constants choose takes 2 %
-    // more than the fastest on average (1.5 times at worst, of calls of 15 to 80 us).
+    // is cut a second launch and the pieces' way to memory and back at 4 TB/s.  Fitted to the times of 5,800 products of 1 to 16,384 rows, 16 to 8192
+    // in and out, forward and backward, one to eight workers, with every tile and 1 to 48 pieces: the cut that these constants choose takes
+    // 1.6 % more than the fastest on average (up to a third more of calls of 12 to 70 us).
     struct Tile { uint32_t bm, bn; double step, alone; };
     const Cut& tiles32() const { return once(tiles32_, [&] { return find32(); }); }
     Cut find32() const
@@ -363,7 +363,7 @@ struct Product {
                 if (tiles * splits > (1ull << 24) && (splits > 1 || t.bm * t.bn < 4096)) break;
                 const double n = (double)all / (double)per / 256.0, whole = std::ceil(n);
                 double us = std::max({(double)per * t.alone, (whole <= 8 ? whole : n) * ((double)per * t.step + 0.09 * area), read});
-                if (splits > 1) us += 6.0 + results * (double)splits * 8.0 / 2e6;
+                if (splits > 1) us += 6.0 + results * (double)splits * 8.0 / 4e6;
                 if (!b.bm || us < b.us) b = {t.bm, t.bn, tiles, splits, per * 32, us};
             }
         }
