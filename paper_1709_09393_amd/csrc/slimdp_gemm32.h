@@ -87,8 +87,9 @@ template <bool KROWS, uint32_t X> struct Tile32 {
 // 117 us instead of 127; 2048 x 4096 x 4096 the same either way).
 //
 // Bound by the matrix unit: 2048 x 4096 x 4096 522 us (132 TFLOP/s; a library product 531 on that machine, 465 on another), 1024 x 1024 x 1024
-// 25 us (24).  Tiles are no larger than 64 x 64 because more blocks leave less of the last round empty (1529 x 832 x 3119: 92 us
-// with 128 x 64, 78 so), and narrower where the result is: 13,286 x 6638 x 16 80 us with 64 x 16 (155 with the square tiles of an earlier kernel); 24 x 3592 x 4608 22 us
+// 25 us (24).  Tiles are no larger than 64 x 64 or 128 x 32 because more blocks leave less of the last round empty (1529 x 832 x 3119: 92 us
+// with 128 x 64, 78 with 64 x 64), and narrower where the result is or where it ends a little behind a tile (11,202 x 2480 x 321: 167 us with
+// 128 x 32, 195 with 32 x 64): 13,286 x 6638 x 16 80 us with 64 x 16 (155 with the square tiles of an earlier kernel); 24 x 3592 x 4608 22 us
 // with 32 x 64.  Few rows are bound by memory, and so is what has few of k.
 // grid: a.blocks, over two dimensions where one does not number them
 template <bool AK, bool BK_, int EPI, uint32_t BM, uint32_t BN, uint32_t WM, uint32_t WN, bool LONG>

@@ -349,7 +349,7 @@ struct Product {
     const Cut& tiles32() const { return once(tiles32_, [&] { return find32(); }); }
     Cut find32() const
     {
-        static const Tile list[] = {{64, 64, 0.42, 0.47}, {32, 64, 0.24, 0.47}, {32, 32, 0.135, 0.16}, {16, 64, 0.18, 0.18}, {64, 16, 0.18, 0.18}};
+        static const Tile list[] = {{64, 64, 0.42, 0.47}, {128, 32, 0.44, 0.6}, {32, 64, 0.24, 0.47}, {32, 32, 0.135, 0.16}, {16, 64, 0.18, 0.18}, {64, 16, 0.18, 0.18}};
         const uint64_t steps = ceil_div(K, 32);
         Cut b{};
         for (const Tile& t : list) {
@@ -463,6 +463,7 @@ template <bool AK, bool BK, int EPI> int product(Call& c, GemmArgs a, const Prod
         };
         if (cut.bm == 64 && cut.bn == 64 && std::min(cut.piece, p.K) <= 256) launch(k_gemm32<AK, BK, EPI, 64, 64, 2, 2, false>);
         else if (cut.bm == 64 && cut.bn == 64) launch(k_gemm32<AK, BK, EPI, 64, 64, 2, 2, true>);
+        else if (cut.bm == 128) launch(k_gemm32<AK, BK, EPI, 128, 32, 4, 1, true>);
         else if (cut.bm == 32 && cut.bn == 64) launch(k_gemm32<AK, BK, EPI, 32, 64, 1, 4, true>);
         else if (cut.bm == 32) launch(k_gemm32<AK, BK, EPI, 32, 32, 2, 2, true>);
         else if (cut.bm == 16) launch(k_gemm32<AK, BK, EPI, 16, 64, 1, 4, true>);
