@@ -306,7 +306,7 @@ struct Product {
     Cut cut(const Kernel& k, uint64_t want, uint64_t all) const
     {
         const uint64_t bk = 128 / es, steps = ceil_div(K, bk), per = std::max<uint64_t>(1, ceil_div(steps, want));
-        const uint64_t splits = std::max<uint64_t>(1, ceil_div(steps, per)), blocks = ceil_div(all, per);
+        const uint64_t splits = std::max<uint64_t>(1, ceil_div(steps, per)), blocks = blocks_of(all, steps, per, splits);
         const double step = blocks <= 256 ? k.alone : k.step;
         // blocks of workers with shorter sums fill the last round up: what all of them take counts, not whole rounds of the longest
         const double rounds = uneven ? std::max(1.0, (double)all / (double)per / k.slots) : (double)ceil_div(blocks, k.slots);
@@ -320,6 +320,11 @@ struct Product {
         uint64_t n = 0;
         for (uint32_t q = 0; q < W; ++q) n += rows_of_k ? std::max<uint64_t>(1, ceil_div(rows[q], bk)) : ceil_div(rows[q], bm);
         return n * ceil_div(N, bn) * (rows_of_k ? ceil_div(M, bm) : ceil_div(K, bk));
+    }
+    // Blocks of all workers; of sums of different lengths as many whole ones as their steps make.
+    uint64_t blocks_of(uint64_t all, uint64_t steps, uint64_t per, uint64_t splits) const
+    {
+        return uneven ? ceil_div(all, per) : all / std::max<uint64_t>(1, steps) * splits;
     }
     Cut best(const Kernel& big, const Kernel& small) const
     {
@@ -354,15 +359,15 @@ struct Product {
         Cut b{};
         for (const Tile& t : list) {
             const uint64_t all = steps_of_all(t.bm, t.bn, 32), tiles = rows_of_k ? W * ceil_div(M, t.bm) * ceil_div(N, t.bn) : all / std::max<uint64_t>(1, steps);
-            const double area = t.bm * t.bn / 4096.0, read = (double)all * (t.bm + t.bn) * 128.0 / 18e6;
+            const double area = t.bm * t.bn / 4096.0;
             uint64_t last = 0;
             for (const uint64_t want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48}) {
                 const uint64_t per = std::max<uint64_t>(1, ceil_div(steps, want)), splits = std::max<uint64_t>(1, ceil_div(steps, per));
                 if (splits == last) continue;
                 last = splits;
                 if (tiles * splits > (1ull << 24) && (splits > 1 || t.bm * t.bn < 4096)) break;
-                const double n = (double)all / (double)per / 256.0, whole = std::ceil(n);
-                double us = std::max({(double)per * t.alone, (whole <= 8 ? whole : n) * ((double)per * t.step + 0.09 * area), read});
+                const double n = (double)blocks_of(all, steps, per, splits) / 256.0, whole = std::ceil(n), each = (double)per;
+                double us = std::max({each * t.alone, (whole <= 8 ? whole : n) * (each * t.step + 0.09 * area), n * each * (t.bm + t.bn) * 32768.0 / 18e6});
                 if (splits > 1) us += 6.0 + results * (double)splits * 8.0 / 4e6;
                 if (!b.bm || us < b.us) b = {t.bm, t.bn, tiles, splits, per * 32, us};
             }
